@@ -287,6 +287,78 @@ lh_status lh_attention_bwd_indexed(const lh_problem* pr, const void* q, const vo
                                    const void* os, const float* lse, const void* dout, void* dq,
                                    void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------- serving: a paged K/V cache and attention over it ---------------- */
+/* The method trains with the hierarchy and resumes with dense attention, whose model is the one that
+   is served (Sec. 5.2; the symmetric pooling of queries cannot decode, App. C.1). These calls serve it:
+   a step takes in new tokens of up to R requests (whole prompts, chunks of prompts, drafted
+   tokens, one token of a running request, in any mix), keeps their K and V rows in pages, and
+   attends with each over its request's cache.
+
+   A cache is a pool of `pages` pages of `page` tokens. kpages, vpages: [pages, Hkv, page, D] (dtype).
+   Token j of request r lies in page table[r][j / page], at j % page; its slot is
+   table[r][j / page] * page + j % page. A step's rows are packed: request r has rows
+   cu_q[r] .. cu_q[r+1] - 1 of q, k, v and o, which are its last tokens.
+
+     table  [R, max_blocks] int32     cu_q [R+1] int32     kv_len [R] int32 (tokens with the step's)
+     q, o   [T, Hq, D]    k, v [T, Hkv, D]    lse [T, Hq] float    slots, pos [T] int32
+
+   Tables and lengths are read on the device: nothing of a step is known to the host but its bounds,
+   so a captured call serves other steps of the same bounds. The int32 arrays need 4-byte alignment.
+   q, k and v may have a stride from token to token (slices of a fused projection), in elements, a
+   multiple of 16 bytes and at least H * D. */
+typedef struct {
+  int32_t R;           /* requests of a step, 1 .. 4096                                            */
+  int32_t max_blocks;  /* columns of the table, >= 1: a request holds max_blocks * page tokens      */
+  int64_t T;           /* rows of q, k, v, o, >= 1 (rows behind the last request's are not touched) */
+  int64_t pages;       /* pages of the cache, >= 1; pages * page < 2^31                             */
+  int32_t page;        /* tokens of a page: a power of two, 16 .. 1024; max_blocks * page < 2^31   */
+  int32_t Hq, Hkv;     /* heads, Hq % Hkv == 0 (query head hq reads KV head hq / (Hq / Hkv)); T * Hq < 2^31 */
+  int32_t D;           /* head dimension: 64 or 128                                                */
+  int32_t dtype;       /* lh_dtype of q, k, v, o and the pages                                     */
+  float scale;         /* softmax scale, finite and >= 0; 0 selects 1/sqrt(D)                      */
+} lh_paged;
+
+/* Validates the bounds of a step (the rules above). Host only. */
+lh_status lh_paged_check(const lh_paged* pc);
+/* Bytes of device workspace that lh_sdpa_paged needs for steps of these bounds. Host only. */
+lh_status lh_paged_workspace_bytes(const lh_paged* pc, size_t* bytes);
+
+/* Block tables, slot maps and lengths of a step. Request r has cached[r] tokens in the cache (the
+   first ceil(cached[r] / page) entries of its table row are its pages) and brings fresh[r] new
+   ones. Its further pages are taken from the end of free_pages[0 .. n_free[0]), in the order of
+   the requests. A request is admitted whole or not at all: it waits if a length is negative, if it
+   would outgrow its table row, if its rows end behind T, or if the pages do not suffice (from the first
+   request that lacks pages on, no request that needs one gets any; those that need none go on).
+   Writes the new entries of table; cu_q[r], the sum of the fresh counts before r (clipped at T);
+   kv_len[r] = cached[r] + fresh[r], or 0 for a request that waits; slots[t] and pos[t] of the tokens, -1 where
+   the request waits and behind the last request; n_left[0], what is left of n_free[0]. A page id of
+   free_pages or table outside [0, pages) gives the slot -1. free_pages holds `pages` entries. */
+lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t* fresh,
+                       const int32_t* free_pages, const int32_t* n_free, int32_t* table,
+                       int32_t* cu_q, int32_t* kv_len, int32_t* slots, int32_t* pos,
+                       int32_t* n_left, void* stream);
+
+/* Writes K and V rows t into slot slots[t] of the pages, for every t < T. A slot outside
+   [0, pages * page) is passed over; every other row of the pages stays as it was. A slot that
+   occurs twice holds an unspecified mix of the two rows. Bitwise copies. */
+lh_status lh_page_write(const lh_paged* pc, const void* k, int64_t k_stride, const void* v,
+                        int64_t v_stride, const int32_t* slots, void* kpages, void* vpages,
+                        void* stream);
+
+/* Attention of the step's rows over the cache: row cu_q[r] + i of request r, whose position is
+   kv_len[r] - (cu_q[r+1] - cu_q[r]) + i, attends to the request's tokens up to that position:
+   o = softmax(scale q K^T) V and lse, the natural-log log-sum-exp of its scaled logits
+   (may be NULL). Logits, statistics and sums in fp32. A row without a token (a request that waits) gets o = 0
+   and lse = -inf. Cached rows that no query row may see (behind kv_len, of other requests, after
+   the row itself) have no effect on it, whatever they hold. Entries of table outside
+   [0, pages) and lengths beyond the table are clamped (no out-of-range read; what such a
+   request's rows get is unspecified), and so are entries of cu_q outside [0, T].
+   ws: at least lh_paged_workspace_bytes() bytes. Deterministic. */
+lh_status lh_sdpa_paged(const lh_paged* pc, const void* q, int64_t q_stride, const void* kpages,
+                        const void* vpages, const int32_t* table, const int32_t* cu_q,
+                        const int32_t* kv_len, void* o, float* lse, void* ws, size_t ws_bytes,
+                        void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,6 +23,8 @@ __all__ = [
     "lh_sdpa_bwd_indexed", "lh_attention_fwd_indexed", "lh_attention_bwd_indexed", "workspace",
     "attention_forward", "attention_backward", "attention_forward_indexed", "attention_backward_indexed",
     "selection_heads",
+    "lh_paged", "paged", "lh_paged_check", "lh_paged_workspace_bytes", "lh_page_plan", "lh_page_write", "lh_sdpa_paged",
+    "paged_workspace", "paged_cache", "page_plan", "attention_paged",
     "library_path", "EXPORTED",
 ]
 
@@ -42,7 +44,8 @@ EXPORTED = [
     "lh_pool_score", "lh_select_topk", "lh_gather", "lh_sdpa_fwd", "lh_sdpa_bwd", "lh_sdpa_bwd_noalloc",
     "lh_scatter", "lh_scatter_bwd",
     "lh_gather_bwd", "lh_attention_fwd", "lh_attention_bwd", "lh_sdpa_fwd_indexed", "lh_sdpa_bwd_indexed",
-    "lh_attention_fwd_indexed", "lh_attention_bwd_indexed",
+    "lh_attention_fwd_indexed", "lh_attention_bwd_indexed", "lh_paged_check", "lh_paged_workspace_bytes",
+    "lh_page_plan", "lh_page_write", "lh_sdpa_paged",
 ]
 
 
@@ -68,6 +71,25 @@ def problem(B, N, Hq, Hkv, D, p, L, k, dtype=LH_BF16, scale=0.0, flags=0) -> lh_
     return lh_problem(B, N, Hq, Hkv, D, p, L, k, dtype, scale, flags)
 
 
+class lh_paged(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("T", ctypes.c_int64),
+                ("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("Hq", ctypes.c_int32),
+                ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+    def __repr__(self):
+        return ("lh_paged(R=%d, max_blocks=%d, T=%d, pages=%d, page=%d, Hq=%d, Hkv=%d, D=%d, dtype=%d, scale=%g)"
+                % (self.R, self.max_blocks, self.T, self.pages, self.page, self.Hq, self.Hkv, self.D, self.dtype,
+                   self.scale))
+
+
+def paged(R, max_blocks, T, pages, page, Hq, Hkv, D, dtype=LH_BF16, scale=0.0) -> lh_paged:
+    """The bounds of serving steps over a paged cache (include/lighthouse.h)."""
+    if isinstance(dtype, torch.dtype):
+        dtype = {torch.float32: LH_F32, torch.bfloat16: LH_BF16}[dtype]
+    return lh_paged(R, max_blocks, T, pages, page, Hq, Hkv, D, dtype, scale)
+
+
 _lib = None
 
 
@@ -79,7 +101,7 @@ def _load():
         raise LighthouseError(
             f"{library_path} is not built; build it with `python -m paper_2605_06554_amd.build`")
     lib = ctypes.CDLL(library_path)
-    P, PR = ctypes.c_void_p, ctypes.POINTER(lh_problem)
+    P, PR, PC = ctypes.c_void_p, ctypes.POINTER(lh_problem), ctypes.POINTER(lh_paged)
     i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     sigs = {
         "lh_check": (i32, [PR]),
@@ -107,6 +129,11 @@ def _load():
         "lh_sdpa_bwd_indexed": (i32, [PR, P, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "lh_attention_fwd_indexed": (i32, [PR, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "lh_attention_bwd_indexed": (i32, [PR, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "lh_paged_check": (i32, [PC]),
+        "lh_paged_workspace_bytes": (i32, [PC, ctypes.POINTER(sz)]),
+        "lh_page_plan": (i32, [PC, P, P, P, P, P, P, P, P, P, P, P]),
+        "lh_page_write": (i32, [PC, P, i64, P, i64, P, P, P, P]),
+        "lh_sdpa_paged": (i32, [PC, P, i64, P, P, P, P, P, P, P, P, sz, P]),
     }
     for name, (res, args) in sigs.items():
         f = getattr(lib, name)
@@ -130,6 +157,10 @@ def _stream(stream):
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _device():
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
 
 
 def _nbytes(t):
@@ -359,6 +390,97 @@ def lh_attention_bwd_indexed(pr, q, k, v, qpyr, kpyr, vpyr, idx, slot, os_, lse,
           _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream))
 
 
+# ---------------------------------------------------------------- serving: a paged K/V cache
+
+def lh_paged_check(pc: lh_paged) -> int:
+    return _load().lh_paged_check(ctypes.byref(pc))
+
+
+def lh_paged_workspace_bytes(pc) -> int:
+    out = ctypes.c_size_t(0)
+    _call("lh_paged_workspace_bytes", ctypes.byref(pc), ctypes.byref(out))
+    return out.value
+
+
+def _need_on(fn, t, name, dt, n, dev):
+    """A dense tensor of n elements or more of dtype dt on device dev."""
+    if t is None or isinstance(t, int):
+        return
+    if not t.is_cuda:
+        raise LighthouseError(f"{fn}: {name} is not a device tensor")
+    if t.get_device() != dev:
+        raise LighthouseError(f"{fn}: {name} is on device {t.get_device()}, the current one is {dev}")
+    if not t.is_contiguous():
+        raise LighthouseError(f"{fn}: {name} is not contiguous")
+    if t.dtype != dt:
+        raise LighthouseError(f"{fn}: {name} has dtype {t.dtype}, {dt} expected")
+    if t.numel() < n:
+        raise LighthouseError(f"{fn}: {name} has {t.numel()} elements, {n} needed")
+
+
+def _need_rows(fn, t, name, dt, T, H, D, dev):
+    """[T, H, D] (or more rows) whose rows of H * D elements are dense; the stride between them, in elements."""
+    if t is None or isinstance(t, int):
+        return H * D
+    if not t.is_cuda:
+        raise LighthouseError(f"{fn}: {name} is not a device tensor")
+    if t.get_device() != dev:
+        raise LighthouseError(f"{fn}: {name} is on device {t.get_device()}, the current one is {dev}")
+    if t.dtype != dt:
+        raise LighthouseError(f"{fn}: {name} has dtype {t.dtype}, {dt} expected")
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < T or shape[1] != H or shape[2] != D:
+        raise LighthouseError(f"{fn}: {name} has shape {tuple(shape)}, ({T}, {H}, {D}) needed")
+    if st[2] != 1 or (H > 1 and st[1] != D):
+        raise LighthouseError(f"{fn}: {name} is not contiguous within a token")
+    if shape[0] == 1:
+        return H * D  # the stride of a single row says nothing
+    return st[0]
+
+
+def _xdt(pc):
+    return torch.bfloat16 if pc.dtype == LH_BF16 else torch.float32
+
+
+def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, n_left, stream=None):
+    fn, i32, dev = "lh_page_plan", torch.int32, _device()
+    for t, name, n in ((cached, "cached", pc.R), (fresh, "fresh", pc.R), (free_pages, "free_pages", pc.pages),
+                       (n_free, "n_free", 1), (table, "table", pc.R * pc.max_blocks), (cu_q, "cu_q", pc.R + 1),
+                       (kv_len, "kv_len", pc.R), (slots, "slots", pc.T), (pos, "pos", pc.T), (n_left, "n_left", 1)):
+        _need_on(fn, t, name, i32, n, dev)
+    _call(fn, ctypes.byref(pc), _p(cached), _p(fresh), _p(free_pages), _p(n_free), _p(table), _p(cu_q), _p(kv_len),
+          _p(slots), _p(pos), _p(n_left), _stream(stream))
+
+
+def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
+    """The strides of the C entry point are k's and v's own."""
+    fn, dt, dev = "lh_page_write", _xdt(pc), _device()
+    ks = _need_rows(fn, k, "k", dt, pc.T, pc.Hkv, pc.D, dev)
+    vs = _need_rows(fn, v, "v", dt, pc.T, pc.Hkv, pc.D, dev)
+    n = pc.pages * pc.Hkv * pc.page * pc.D
+    _need_on(fn, slots, "slots", torch.int32, pc.T, dev)
+    _need_on(fn, kpages, "kpages", dt, n, dev)
+    _need_on(fn, vpages, "vpages", dt, n, dev)
+    _call(fn, ctypes.byref(pc), _p(k), ks, _p(v), vs, _p(slots), _p(kpages), _p(vpages), _stream(stream))
+
+
+def lh_sdpa_paged(pc, q, kpages, vpages, table, cu_q, kv_len, o, lse, ws, ws_bytes=None, stream=None):
+    """The stride of the C entry point is q's own; lse may be None."""
+    fn, dt, i32, dev = "lh_sdpa_paged", _xdt(pc), torch.int32, _device()
+    qs = _need_rows(fn, q, "q", dt, pc.T, pc.Hq, pc.D, dev)
+    n = pc.pages * pc.Hkv * pc.page * pc.D
+    _need_on(fn, kpages, "kpages", dt, n, dev)
+    _need_on(fn, vpages, "vpages", dt, n, dev)
+    _need_on(fn, table, "table", i32, pc.R * pc.max_blocks, dev)
+    _need_on(fn, cu_q, "cu_q", i32, pc.R + 1, dev)
+    _need_on(fn, kv_len, "kv_len", i32, pc.R, dev)
+    _need_on(fn, o, "o", dt, pc.T * pc.Hq * pc.D, dev)
+    _need_on(fn, lse, "lse", torch.float32, pc.T * pc.Hq, dev)
+    _need_on(fn, ws, "ws", torch.uint8, ws_bytes or 0, dev)
+    _call(fn, ctypes.byref(pc), _p(q), qs, _p(kpages), _p(vpages), _p(table), _p(cu_q), _p(kv_len), _p(o), _p(lse), _p(ws),
+          _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream))
+
+
 # ---------------------------------------------------------------- allocation helpers
 
 def selection_heads(pr) -> int:
@@ -453,3 +575,34 @@ def attention_backward(pr, state, dout, stream=None):
     lh_attention_bwd(pr, state["idx"], state["slot"], state["qs"], state["ks"], state["vs"], state["os"],
                      state["lse"], dout, dq, dk, dv, ws, stream=stream)
     return dq, dk, dv
+
+
+def paged_workspace(pc, device="cuda"):
+    """A device byte buffer of lh_paged_workspace_bytes(pc) bytes. Calls that may run at the same time (two
+    streams, two captured graphs) need one each."""
+    return torch.empty(max(lh_paged_workspace_bytes(pc), 1), dtype=torch.uint8, device=device)
+
+
+def paged_cache(pages, page, Hkv, D, dtype=torch.bfloat16, device="cuda"):
+    """(kpages, vpages), [pages, Hkv, page, D] each, not initialised (rows that no request holds are never used)."""
+    return tuple(torch.empty(pages, Hkv, page, D, dtype=dtype, device=device) for _ in range(2))
+
+
+def page_plan(pc, cached, fresh, free_pages, n_free, table, stream=None):
+    """Allocates the outputs and runs lh_page_plan. Returns a dict of cu_q, kv_len, slots, pos and n_left; the new
+    entries of table are written in place."""
+    e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)  # noqa: E731
+    out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), n_left=e(1))
+    lh_page_plan(pc, cached, fresh, free_pages, n_free, table, *out.values(), stream=stream)
+    return out
+
+
+def attention_paged(pc, q, k, v, kpages, vpages, table, plan, ws=None, stream=None):
+    """One layer's attention of a step: writes k and v into the cache and attends with q, by the plan of
+    page_plan (the same for every layer of the step). Returns (o, lse)."""
+    lh_page_write(pc, k, v, plan["slots"], kpages, vpages, stream=stream)
+    o = torch.empty(pc.T, pc.Hq, pc.D, dtype=q.dtype, device=q.device)
+    lse = torch.empty(pc.T, pc.Hq, dtype=torch.float32, device=q.device)
+    ws = paged_workspace(pc, q.device) if ws is None else ws
+    lh_sdpa_paged(pc, q, kpages, vpages, table, plan["cu_q"], plan["kv_len"], o, lse, ws, stream=stream)
+    return o, lse

@@ -13,13 +13,21 @@ namespace {
 
 thread_local char g_err[512] = "";
 
-lh_status fail(lh_status s, const char* fmt, ...) {
+}  // namespace
+
+// (declared in lh_common.h: the host code of the paged calls reports through it too)
+lh_status lh_fail(lh_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof(g_err), fmt, ap);
   va_end(ap);
   return s;
 }
+
+namespace {
+
+template <typename... A>
+lh_status fail(lh_status s, const char* fmt, A... a) { return lh_fail(s, fmt, a...); }
 
 constexpr int kMaxLevels = 8;       // kernels are instantiated for L = 1..8
 constexpr int64_t kSelLdsKeys = 32768;        // a level up to this many candidates ranks in LDS

@@ -141,6 +141,9 @@ struct LhShape {
   int64_t maxsel;      // largest candidate count of a level that needs a real top-k
 };
 
+// Sets the thread's error detail (api.cpp) and returns s.
+lh_status lh_fail(lh_status s, const char* fmt, ...);
+
 // Kernel launchers (each returns hipGetLastError() after enqueueing).
 hipError_t lh_launch_pool_score(const LhShape& s, const void* q, const void* k, const void* v,
                                 void* qpyr, void* kpyr, void* vpyr, float* s_qk, float* s_kq,

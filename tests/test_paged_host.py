@@ -1,0 +1,171 @@
+"""The paged calls' refusals, on the host: nothing is launched by any of them."""
+import ctypes
+
+import pytest
+import torch
+
+import paged_ref
+import paper_2605_06554_amd as lh
+
+
+def _pc(**kw):
+    base = dict(R=4, max_blocks=8, T=100, pages=64, page=16, Hq=8, Hkv=2, D=64, dtype=lh.LH_BF16)
+    base.update(kw)
+    return lh.paged(**base)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), 0),
+    (dict(R=0), -2), (dict(R=4096), 0), (dict(R=4097), -2),
+    (dict(T=0), -2), (dict(pages=0), -2), (dict(max_blocks=0), -2),
+    (dict(page=8), -3), (dict(page=24), -3), (dict(page=1024), 0), (dict(page=2048), -3), (dict(page=-16), -3),
+    (dict(Hq=3), -3), (dict(Hkv=0), -3), (dict(Hq=0, Hkv=1), -3), (dict(D=96), -3), (dict(D=0), -3),
+    (dict(dtype=2), -4), (dict(dtype=torch.float32), 0),
+    (dict(scale=float("nan")), -8), (dict(scale=float("inf")), -8), (dict(scale=-1.0), -3), (dict(scale=0.5), 0),
+    (dict(pages=2 ** 27 - 1), 0), (dict(pages=2 ** 27), -2),          # pages * page < 2^31
+    (dict(max_blocks=2 ** 27 - 1), 0), (dict(max_blocks=2 ** 27), -2),
+    (dict(T=2 ** 28 - 1), 0), (dict(T=2 ** 28), -2),                 # T * Hq < 2^31
+])
+def test_check_codes(kw, code):
+    pc = _pc(**kw)
+    assert lh.lh_paged_check(pc) == code
+    if code:
+        assert lh.lh_last_error() != ""
+        with pytest.raises(lh.LighthouseError):
+            lh.lh_paged_workspace_bytes(pc)
+    else:
+        assert lh.lh_paged_workspace_bytes(pc) >= 0
+
+
+def test_null_and_misaligned_pointers():
+    lib, pc = lh._load(), _pc()
+    ok = [0x10000 * (i + 1) for i in range(12)]
+    by = ctypes.byref(pc)
+    assert lib.lh_paged_check(None) == -1
+    assert lib.lh_paged_workspace_bytes(by, None) == -1
+    for i in range(10):  # each pointer of the plan in turn
+        bad = ok[:10]
+        bad[i] = None
+        assert lib.lh_page_plan(by, *bad, None) == -1
+        bad[i] = 0x10002
+        assert lib.lh_page_plan(by, *bad, None) == -5
+    row = 2 * 64
+    for args, code in [((None, row, 0x1000, row, 0x2000, 0x3000, 0x4000), -1),
+                       ((0x1008, row, 0x1000, row, 0x2000, 0x3000, 0x4000), -5),
+                       ((0x1000, row, 0x1000, row, 0x2002, 0x3000, 0x4000), -5),
+                       ((0x1000, row, 0x1000, row, 0x2000, 0x3000, 0x4008), -5),
+                       ((0x1000, row - 8, 0x1000, row, 0x2000, 0x3000, 0x4000), -2),
+                       ((0x1000, row, 0x1000, row + 4, 0x2000, 0x3000, 0x4000), -5),
+                       ((0x1000, row, 0x1000, 2 ** 41, 0x2000, 0x3000, 0x4000), -2),
+                       ((0x1000, 0, 0x1000, row, 0x2000, 0x3000, 0x4000), -2),
+                       ((0x1000, -row, 0x1000, row, 0x2000, 0x3000, 0x4000), -2)]:
+        assert lib.lh_page_write(by, *args, None) == code, (args, lh.lh_last_error())
+    need = lh.lh_paged_workspace_bytes(pc)
+    good = [0x1000, 8 * 64, 0x2000, 0x3000, 0x4000, 0x5000, 0x6000, 0x7000, 0x8000, 0x10000, need]
+    for i, value, code in [(0, None, -1), (0, 0x1008, -5), (1, 8 * 64 - 8, -2), (1, 8 * 64 + 1, -5), (2, None, -1),
+                           (3, 0x3004, -5), (4, None, -1), (4, 0x4002, -5), (5, None, -1), (6, 0x6001, -5),
+                           (7, None, -1), (7, 0x7008, -5), (8, 0x8002, -5)]:
+        bad = list(good)
+        bad[i] = value
+        assert lib.lh_sdpa_paged(by, *bad, None) == code, (i, value, lh.lh_last_error())
+    if need:
+        for i, value, code in [(9, None, -6), (9, 0x10010, -5), (10, need - 1, -6)]:
+            bad = list(good)
+            bad[i] = value
+            assert lib.lh_sdpa_paged(by, *bad, None) == code
+    assert lib.lh_sdpa_paged(ctypes.byref(_pc(D=32)), *good, None) == -3
+
+
+class _Fake:
+    """Stands in for a device tensor (only what the binding reads)."""
+
+    def __init__(self, shape, dtype, stride=None, device=0):
+        self.shape, self.dtype, self.is_cuda, self._device = tuple(shape), dtype, True, device
+        dense, n = [], 1
+        for x in reversed(self.shape):
+            dense.insert(0, n)
+            n *= x
+        self._stride, self._n, self._dense = tuple(stride or dense), n, stride is None
+
+    def numel(self):
+        return self._n
+
+    def stride(self):
+        return self._stride
+
+    def is_contiguous(self):
+        return self._dense
+
+    def get_device(self):
+        return self._device
+
+    def data_ptr(self):
+        raise AssertionError("a refused call reads no address")
+
+
+def _refused(call, args, i, bad, msg):
+    args = list(args)
+    args[i] = bad
+    with pytest.raises(lh.LighthouseError, match=msg):
+        call(*args)
+
+
+def test_binding_refuses_bad_tensors():
+    pc, i32, bf = _pc(), torch.int32, torch.bfloat16
+    plan = [pc, _Fake([4], i32), _Fake([4], i32), _Fake([64], i32), _Fake([1], i32), _Fake([4, 8], i32), _Fake([5], i32),
+            _Fake([4], i32), _Fake([100], i32), _Fake([100], i32), _Fake([1], i32)]
+    for i, n in ((1, 4), (2, 4), (3, 64), (5, 32), (6, 5), (7, 4), (8, 100), (9, 100)):
+        _refused(lh.lh_page_plan, plan, i, _Fake([n - 1], i32), "elements")
+        _refused(lh.lh_page_plan, plan, i, _Fake([n], torch.int64), "dtype")
+        _refused(lh.lh_page_plan, plan, i, _Fake([n], i32, device=1), "device 1")
+    _refused(lh.lh_page_plan, plan, 5, _Fake([4, 8], i32, stride=(16, 1)), "not contiguous")
+    _refused(lh.lh_page_plan, plan, 1, torch.zeros(4, dtype=i32), "not a device tensor")
+    pool = _Fake([64, 2, 16, 64], bf)
+    write = [pc, _Fake([100, 2, 64], bf), _Fake([100, 2, 64], bf), _Fake([100], i32), pool, pool]
+    for i in (1, 2):
+        _refused(lh.lh_page_write, write, i, _Fake([99, 2, 64], bf), "shape")
+        _refused(lh.lh_page_write, write, i, _Fake([100, 128], bf), "shape")
+        _refused(lh.lh_page_write, write, i, _Fake([100, 2, 64], bf, stride=(64, 6400, 1)), "within a token")
+        _refused(lh.lh_page_write, write, i, _Fake([100, 2, 64], torch.float32), "dtype")
+        _refused(lh.lh_page_write, write, i, _Fake([100, 2, 64], bf, device=3), "device 3")
+    _refused(lh.lh_page_write, write, 4, _Fake([63, 2, 16, 64], bf), "elements")
+    attend = [pc, _Fake([100, 8, 64], bf), pool, pool, _Fake([4, 8], i32), _Fake([5], i32), _Fake([4], i32),
+              _Fake([100, 8, 64], bf), _Fake([100, 8], torch.float32), _Fake([1 << 30], torch.uint8)]
+    for i, bad, msg in ((1, _Fake([100, 4, 64], bf), "shape"), (2, _Fake([64, 2, 16, 32], bf), "elements"),
+                        (3, _Fake([64, 2, 16, 64], torch.float16), "dtype"), (4, _Fake([4, 7], i32), "elements"),
+                        (5, _Fake([4], i32), "elements"), (6, _Fake([3], i32), "elements"),
+                        (7, _Fake([99, 8, 64], bf), "elements"), (8, _Fake([100, 8], bf), "dtype"),
+                        (9, _Fake([16], i32), "dtype"), (7, _Fake([100, 8, 64], bf, device=1), "device 1")):
+        _refused(lh.lh_sdpa_paged, attend, i, bad, msg)
+
+
+def test_reference_plan_hands_out_pages_in_order():
+    """The oracle of the plan itself, on a case worked by hand: pages of 16; request 0 fills its page and takes one;
+    request 1 brings nothing; request 2 lacks pages and waits; request 3 needs none and goes on; request 4 waits."""
+    table = [[7, -1, -1], [3, -1, -1], [-1] * 3, [5, -1, -1], [-1] * 3]
+    got = paged_ref.plan([10, 16, 0, 1, 0], [8, 0, 33, 2, 1], [20, 21, 22, 99], 3, table, 16, 64, 44)
+    t, cu, kv, slots, pos, left = got
+    assert t == [[7, 22, -1], [3, -1, -1], [-1] * 3, [5, -1, -1], [-1] * 3]
+    assert cu == [0, 8, 8, 41, 43, 44] and kv == [18, 16, 0, 3, 0] and left == 2
+    assert slots[:8] == [7 * 16 + x for x in range(10, 16)] + [22 * 16, 22 * 16 + 1]
+    assert slots[8:41] == [-1] * 33 and slots[41:] == [81, 82, -1] and pos[41:] == [1, 2, -1]
+
+
+def test_reference_attention_is_the_definition():
+    """The oracle of the attention against a loop over keys, on pages in a mixed order, with an empty row."""
+    g = torch.Generator().manual_seed(5)
+    q = torch.randn(5, 2, 64, generator=g).to(torch.bfloat16)
+    kp, vp = (torch.randn(6, 1, 16, 64, generator=g).to(torch.bfloat16) for _ in range(2))
+    table, cu, kv = [[4, 1], [2, 0]], [0, 3, 5], [18, 1]
+    o, lse, _, _ = paged_ref.attend(q, kp, vp, table, cu, kv, 16)
+    for r, t, keys in ((0, 0, 16), (0, 2, 18), (1, 3, 0), (1, 4, 1)):
+        for h in range(2):
+            rows = [(table[r][j // 16], j % 16) for j in range(keys)]
+            x = [float(q[t, h].double() @ kp[a, 0, b].double()) / 8 for a, b in rows]
+            if not x:
+                assert bool((o[t, h] == 0).all()) and float(lse[t, h]) == float("-inf")
+                continue
+            w = torch.tensor(x, dtype=torch.float64).softmax(0)
+            ref = sum(p * vp[a, 0, b].double() for p, (a, b) in zip(w, rows))
+            assert torch.allclose(o[t, h], ref, rtol=1e-12, atol=1e-14)
+            assert abs(float(lse[t, h]) - float(torch.tensor(x, dtype=torch.float64).logsumexp(0))) < 1e-12
