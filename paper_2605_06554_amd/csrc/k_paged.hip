@@ -5,23 +5,6 @@
 
 namespace lh {
 
-// Inclusive sum over the workgroup's threads, in thread order, plus `carry`; `part` holds a word per
-// wave. Every thread calls it.
-template <int NT>
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t carry, int64_t* part) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
-  if (lane == 63) part[w] = x;
-  __syncthreads();
-  for (int i = 0; i < w; ++i) carry += part[i];
-  __syncthreads();
-  return x + carry;
-}
-
 __device__ __forceinline__ int64_t blocks_of(int64_t tokens, int shift) {
   return (tokens + ((int64_t)1 << shift) - 1) >> shift;
 }

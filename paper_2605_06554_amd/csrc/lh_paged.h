@@ -3,6 +3,27 @@
 
 #include "lh_common.h"
 
+namespace lh {
+
+// Inclusive sum over the workgroup's threads, in thread order, plus `carry`; `part` holds a word per
+// wave. Every thread calls it.
+template <int NT>
+__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t carry, int64_t* part) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  if (lane == 63) part[w] = x;
+  __syncthreads();
+  for (int i = 0; i < w; ++i) carry += part[i];
+  __syncthreads();
+  return x + carry;
+}
+
+}  // namespace lh
+
 // A step's bounds, checked once per call on the host (include/lighthouse.h: lh_paged).
 struct LhPaged {
   int64_t T, pages;
