@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "liblighthouse.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["api.cpp", "api_paged.cpp", "k_pool_score.hip", "k_select.hip", "k_gather_scatter.hip", "k_sdpa.hip",
-           "k_sdpa_f32.hip", "k_sdpa_mfma.hip", "k_paged.hip", "k_paged_sdpa.hip"]
+           "k_sdpa_f32.hip", "k_sdpa_mfma.hip", "k_paged.hip", "k_paged_sdpa.hip", "k_paged_rows.hip",
+           "k_paged_tile.hip"]
 # measurement probe, a library of its own (not part of the attention path)
 CEILING_SOURCE = "k_ceiling.hip"
 CEILING_OUT = os.path.join(HERE, "libceiling.so")
