@@ -26,6 +26,22 @@ struct TileCfg {
   static constexpr int RPB = 512 / D;                       // rows of one
 };
 
+// lane_offsets of a tile's rows, from three registers: the k-step and the column block change bits of a lane's
+// offset that the swizzle leaves alone or flips, so they come in by an exclusive or. (All 16 held: 16 registers
+// spilled, and a reload in the loop waits for the tile in flight.)
+template <int D>
+struct LaneBase {
+  int row0, trl0, trh0;
+  __device__ __forceinline__ explicit LaneBase(int lane) {
+    const LaneOff<D> o = lane_offsets<D>(lane, 0);
+    row0 = o.row[0], trl0 = o.trl[0], trh0 = o.trh[0];
+  }
+  __device__ __forceinline__ int row(int kk) const { return row0 ^ (kk << 5); }
+  __device__ __forceinline__ int trl(int d) const { return trl0 ^ (d << 6); }
+  __device__ __forceinline__ int trh(int d) const { return trh0 ^ (d << 6); }
+  __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row0), "+v"(trl0), "+v"(trh0)); }  // nothing formed ahead
+};
+
 template <int D, int NW>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(TileCfg<D, NW>::EU, TileCfg<D, NW>::EU)))
 paged_tile(const PagedArgs a) {
@@ -48,7 +64,7 @@ paged_tile(const PagedArgs a) {
     int lane = tid & 63;
     asm volatile("" : "+v"(lane));
     const int hh = lane >> 5, r32 = lane & 31;
-    const LaneOff<D> lo = lane_offsets<D>(lane, 0);
+    LaneBase<D> lo(lane);
     // this lane's row and bytes of the 1 KB blocks that it copies (a block too many repeats another's: same bytes)
     auto block_of = [&](int j) __attribute__((always_inline)) {
       const int b = j * NW + w;
@@ -122,6 +138,7 @@ paged_tile(const PagedArgs a) {
       bf16_t* const Kt = SL ? Ks1 : Ks0;
       bf16_t* const Vt = SL ? Vs1 : Vs0;
       sync_tiles<0>();  // tile kt landed in every wave; tile kt - 1 is done
+      lo.fresh();
       const int k0 = kt * FK;
       // Values of V that are not finite may be of keys that some rows see and others do not, and 0 times them
       // is NaN: all waves look for them where a row of the tile is masked, and take them out.
@@ -155,7 +172,7 @@ paged_tile(const PagedArgs a) {
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb) sacc[kb] = mfma32(row8(Kt, kb * 32 * RB + lo.row[kk]), qreg[kk], sacc[kb]);
+          for (int kb = 0; kb < 2; ++kb) sacc[kb] = mfma32(row8(Kt, kb * 32 * RB + lo.row(kk)), qreg[kk], sacc[kb]);
         if (k0 + FK - 1 > wsafe) {
           const int sees = pos - k0 - 4 * hh;  // (against constants: 32 keys a lane held across the loop were spilled)
 #pragma unroll
@@ -200,7 +217,7 @@ paged_tile(const PagedArgs a) {
         if (st + 1 < 4) pnext = soft(st + 1);
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
-          oacc[d] = mfma32(tr8(Vt, 16 * st * RB + lo.trl[d], 16 * st * RB + lo.trh[d]), pcur, oacc[d]);
+          oacc[d] = mfma32(tr8(Vt, 16 * st * RB + lo.trl(d), 16 * st * RB + lo.trh(d)), pcur, oacc[d]);
         if (st + 1 < 4) {
           // groups: DS reads (mask 0x100), MFMA (0x008), VALU (0x002), transcendental (0x400)
           __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
@@ -226,10 +243,6 @@ paged_tile(const PagedArgs a) {
       // What was taken out is added to the rows that see its key: the masked tiles once more, with codes in V's
       // place (1 for +inf, 64 for -inf, 4096 for NaN). A product with the rows' view of the keys (1 or 0) counts
       // them, 16 keys at a time, so that the counts do not overlap.
-      int l2 = lane;
-      asm volatile("" : "+v"(l2));  // (as above)
-      const LaneOff<D> lo2 = lane_offsets<D>(l2, 0);
-      const int h2 = l2 >> 5;
       for (int kt = safe / FK > t0 ? safe / FK : t0; kt < t1; ++kt) {
         __syncthreads();
         next_pages(kt);
@@ -245,12 +258,12 @@ paged_tile(const PagedArgs a) {
         for (int st = 0; st < 4; ++st) {
           float see[8];
 #pragma unroll
-          for (int y = 0; y < 8; ++y) see[y] = 8 * (y >> 2) + (y & 3) <= pos - kt * FK - 16 * st - 4 * h2 ? 1.0f : 0.0f;
+          for (int y = 0; y < 8; ++y) see[y] = 8 * (y >> 2) + (y & 3) <= pos - kt * FK - 16 * st - 4 * hh ? 1.0f : 0.0f;
           const bf16x8 s8 = cvt8(see);
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) {
             __builtin_amdgcn_sched_barrier(0);
-            const f32x16 cnt = mfma32(tr8(Vs0, 16 * st * RB + lo2.trl[d], 16 * st * RB + lo2.trh[d]), s8, f32x16{});
+            const f32x16 cnt = mfma32(tr8(Vs0, 16 * st * RB + lo.trl(d), 16 * st * RB + lo.trh(d)), s8, f32x16{});
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int c = (int)cnt[i];
