@@ -17,8 +17,8 @@
 //   permutes the columns of O^T and not the sums, and hands a lane consecutive columns to store.
 //   fp32, MFMA 16x16x4: A[m = n][k = g] one value; the k order of step c of 4 is column 16 kk + 4 g + c (a
 //   16-byte read), and of V step i the key 4 g + i, whose columns need no transpose at all.
-// The loads of the next block's K are issued when the last ones were multiplied, the same for V, and
-// 12 waves a CU hide one another's latency.
+// The loads of the next block's K are issued when the last ones were multiplied, the same for V; 8 waves a CU keep
+// enough of them in flight (64 requests, 482,000 keys: 312 us with 8 waves, 325 with 12, 327 with 4).
 #include <math.h>
 
 #include "lh_mfma.h"
@@ -36,9 +36,15 @@ struct RowsCfg {
   static constexpr int KV = KB / 16 * D / (sizeof(T) == 2 ? 32 : 16);         // 16-byte reads of K a lane and block
   static constexpr int NV = KB / 4;                                           // keys of V a lane and block
   static constexpr int VW = DL * sizeof(T) / 4;                               // 32-bit words of one of them
-  static constexpr int EU = RT == 1 ? 3 : 2;  // workgroups a CU
+  static constexpr int EU = 2;  // workgroups a CU
   static constexpr int64_t W = 256 * EU;
 };
+
+template <bool NT, typename V>
+__device__ __forceinline__ V load(const char* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
 
 template <typename T, int D, int RT>
 struct Wave {
@@ -50,7 +56,8 @@ struct Wave {
   uint32_t v[C::NV][C::VW];
 };
 
-template <typename T, int D, int RT>
+// NT: K and V are loaded with the non-temporal hint.
+template <typename T, int D, int RT, bool NT>
 __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const PagedArgs a) {
   using C = RowsCfg<T, D, RT>;
   constexpr int TM = C::TM, DL = C::DL, KB = C::KB, RB = D * (int)sizeof(T);
@@ -58,29 +65,31 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
   constexpr int LD = D + 4;  // a row of the LDS parts, padded by 16 bytes
   __shared__ __align__(16) float parts[C::NW][16][LD];
   __shared__ float ms[C::NW][16], ls[C::NW][16];
-  __shared__ int64_t scan[C::NW], found[2];
+  __shared__ int64_t scan[C::NW];
+  __shared__ typename Walk<TM, 16>::Found found;
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6), n = lane & 15, g = lane >> 4;
 
   Walk<TM, 16> wk;
-  if (!wk.template begin<256>(a, scan, found)) return;
+  if (!wk.template begin<256>(a, scan, &found)) return;
   Wave<T, D, RT> s;
   do {
-    const Req<TM, 16>& rq = wk.rq;
-    const int r = wk.r, h = wk.h, row0 = wk.t * TM, rows = rq.rows - row0 < TM ? rq.rows - row0 : TM;
-    const int keys = rq.base + (row0 + rows - 1) / a.G + 1;  // that any row of the tile sees
-    const int safe = rq.base + row0 / a.G + 1;               // that all of them see
+    const int first = uni(wk.rq.first), base = uni(wk.rq.base), all_rows = uni(wk.rq.rows);
+    const int r = uni(wk.r), h = uni(wk.h), row0 = uni(wk.t) * TM, rows = all_rows - row0 < TM ? all_rows - row0 : TM;
+    const int keys = uni(base + (row0 + rows - 1) / a.G + 1);  // that any row of the tile sees
+    const int safe = uni(base + row0 / a.G + 1);               // that all of them see
     int b0, b1;
     wk.blocks(keys > 0 ? (keys + KB - 1) / KB : 0, b0, b1);
+    b0 = uni(b0), b1 = uni(b1);
 
     // ---- this wave's blocks
     int pos[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       int row = row0 + rt * 16 + n;
-      row = row < rq.rows ? row : rq.rows - 1;
+      row = row < all_rows ? row : all_rows - 1;
       const int tok = row / a.G;
-      pos[rt] = rq.base + tok;
-      const T* qp = (const T*)a.q + (int64_t)(rq.first + tok) * a.q_stride + (int64_t)(h * a.G + row - tok * a.G) * D;
+      pos[rt] = base + tok;
+      const T* qp = (const T*)a.q + (int64_t)(first + tok) * a.q_stride + (int64_t)(h * a.G + row - tok * a.G) * D;
 #pragma unroll
       for (int c = 0; c < RB / 64; ++c) s.q[rt][c] = *reinterpret_cast<const u32v4*>((const char*)qp + c * 64 + g * 16);
       s.m[rt] = -INFINITY, s.l[rt] = 0.0f;
@@ -89,35 +98,44 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
     }
     const int64_t ids = (int64_t)r * a.max_blocks;  // the request's row of the table
     const int last = (keys - 1) >> a.shift;  // the last page in use (keys > 0 wherever it is used)
-    auto at = [&](int j) __attribute__((always_inline)) {  // bytes from the pool's start to 16 keys from j
-      int b_ = j >> a.shift;
-      b_ = b_ < last ? b_ : last;
-      const int32_t id = page_id(a.table, ids + b_, a.pages);
-      return ((((int64_t)id * a.Hkv + h) << a.shift) + (j & ((1 << a.shift) - 1))) * RB;
-    };
-    auto load_k = [&](int j) __attribute__((always_inline)) {
+    // A block's pages are looked up a block ahead of its loads; K and V lie at the same place of their pools.
+    int32_t pg[KB / 16];
+    int64_t off[KB / 16];  // bytes from the pool's start to 16 keys
+    auto look_up = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
       for (int c = 0; c < KB / 16; ++c) {
-        const char* p = (const char*)a.kp + at(j + 16 * c);
-#pragma unroll
-        for (int i = 0; i < RB / 64; ++i)
-          s.k[c * (RB / 64) + i] = *reinterpret_cast<const u32v4*>(p + n * RB + g * 16 + i * 64);
+        const int b = (j + 16 * c) >> a.shift;
+        pg[c] = page_id(a.table, ids + (b < last ? b : last), a.pages);
       }
     };
-    auto load_v = [&](int j) __attribute__((always_inline)) {
+    auto place = [&](int j) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < KB / 16; ++c)
+        off[c] = ((((int64_t)pg[c] * a.Hkv + h) << a.shift) + ((j + 16 * c) & ((1 << a.shift) - 1))) * RB;
+    };
+    auto load_k = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int c = 0; c < KB / 16; ++c) {
-        const char* p = (const char*)a.vp + at(j + 16 * c);
+        const char* p = (const char*)a.kp + off[c];
+#pragma unroll
+        for (int i = 0; i < RB / 64; ++i)
+          s.k[c * (RB / 64) + i] = load<NT, u32v4>(p + n * RB + g * 16 + i * 64);
+      }
+    };
+    auto load_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < KB / 16; ++c) {
+        const char* p = (const char*)a.vp + off[c];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const char* pv = p + (4 * g + i) * RB + n * (DL * (int)sizeof(T));
           if constexpr (C::VW == 2) {
-            const u32v2 y = *reinterpret_cast<const u32v2*>(pv);
+            const u32v2 y = load<NT, u32v2>(pv);
             s.v[4 * c + i][0] = y[0], s.v[4 * c + i][1] = y[1];
           } else {
 #pragma unroll
             for (int z = 0; z < C::VW / 4; ++z) {
-              const u32v4 y = *reinterpret_cast<const u32v4*>(pv + 16 * z);
+              const u32v4 y = load<NT, u32v4>(pv + 16 * z);
 #pragma unroll
               for (int o = 0; o < 4; ++o) s.v[4 * c + i][4 * z + o] = y[o];
             }
@@ -204,8 +222,11 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
     };
     int blk = b0 + w;
     if (blk < b1) {
-      load_k(blk * KB);
-      load_v(blk * KB);
+      look_up(blk * KB);
+      place(blk * KB);
+      load_k();
+      load_v();
+      look_up((blk + C::NW) * KB);
     }
     for (; blk < b1; blk += C::NW) {
       const int j0 = blk * KB, next = (blk + C::NW) * KB;
@@ -229,7 +250,11 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
             }
           }
         }
-      if (more) load_k(next);
+      if (more) {
+        place(next);
+        load_k();
+        look_up(next + C::NW * KB);
+      }
       const bool masked = j0 + KB > safe;
       if (masked) {
 #pragma unroll
@@ -283,7 +308,7 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
       }
       if (__any(odd)) odd_values(j0);
       pv(p);
-      if (more) load_v(next);
+      if (more) load_v();
     }
 
     // ---- the four waves joined
@@ -320,7 +345,7 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
         }
         if (whole) {
           const int gr = row0 + row, tok = gr / a.G;
-          const int64_t at_ = (int64_t)(rq.first + tok) * a.Hq + h * a.G + (gr - tok * a.G);
+          const int64_t at_ = (int64_t)(first + tok) * a.Hq + h * a.G + (gr - tok * a.G);
           const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
           T* o = (T*)a.o + at_ * D + c0;
           if constexpr (B16) {
@@ -348,19 +373,23 @@ __global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const
   } while (wk.next(a));
 }
 
-template <typename T, int D, int RT>
-static void launch_rows(const PagedArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((paged_rows<T, D, RT>), dim3((unsigned)RowsCfg<T, D, RT>::W), dim3(256), 0, st, a);
+template <typename T, int D, int RT, bool NT>
+static PagedVariant variant() {
+  using C = RowsCfg<T, D, RT>;
+  return {C::W, C::TM, [](const PagedArgs& a, hipStream_t st) {
+            hipLaunchKernelGGL((paged_rows<T, D, RT, NT>), dim3((unsigned)C::W), dim3(256), 0, st, a);
+          }};
 }
+// A request of one tile reads its keys once, and the non-temporal hint is worth 8% of the time (6.1 against 5.6
+// TB/s, 64 requests of 482,000 keys); one of several finds them in the caches (four tiles, fp32: 60 us, 67 with the hint).
 template <typename T, int D>
-static PagedVariant variant(int rows) {
-  if (rows > 16) return {RowsCfg<T, D, 2>::W, 32, launch_rows<T, D, 2>};
-  return {RowsCfg<T, D, 1>::W, 16, launch_rows<T, D, 1>};
+static PagedVariant variant(int64_t rows) {
+  return rows > 32 ? variant<T, D, 2, false>() : rows > 16 ? variant<T, D, 2, true>() : variant<T, D, 1, true>();
 }
 
 }  // namespace lh
 
-PagedVariant lh_paged_rows_variant(const LhPaged& s, int rows) {
+PagedVariant lh_paged_rows_variant(const LhPaged& s, int64_t rows) {
   if (s.dtype == LH_BF16) return s.D == 128 ? lh::variant<lh::bf16_t, 128>(rows) : lh::variant<lh::bf16_t, 64>(rows);
   return s.D == 128 ? lh::variant<float, 128>(rows) : lh::variant<float, 64>(rows);
 }

@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a, int TM) {
 static PagedVariant variant_of(const LhPaged& s) {
   const int64_t rows = s.T * s.G / s.R;
   if (s.dtype == LH_BF16 && rows > 64) return lh_paged_tile_variant(s, rows > 192 ? 12 : 4);
-  return lh_paged_rows_variant(s, rows > 16 ? 32 : 16);
+  return lh_paged_rows_variant(s, rows);
 }
 
 template <typename T, int D>

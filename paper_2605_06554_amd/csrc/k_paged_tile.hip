@@ -48,14 +48,16 @@ paged_tile(const PagedArgs a) {
   using C = TileCfg<D, NW>;
   constexpr int TM = C::TM, FK = C::FK, RB = 2 * D, NT = 64 * NW, LPW = C::LPW;
   __shared__ __align__(16) bf16_t Ks0[FK * D], Ks1[FK * D], Vs0[FK * D], Vs1[FK * D];
-  __shared__ int64_t scan[NW], found[2];
+  __shared__ int64_t scan[NW];
+  __shared__ typename Walk<TM, 6>::Found found;
+  __shared__ int32_t more;
   const int tid = threadIdx.x, w = uni(tid >> 6);
   // The way along the part waits in LDS while a tile is worked on: in registers (the results of divisions live in
   // vector registers, uniform or not) it made the loop spill 22.
   __shared__ Walk<TM, 6> way;
   {
     Walk<TM, 6> wk;
-    if (!wk.template begin<NT>(a, scan, found)) return;
+    if (!wk.template begin<NT>(a, scan, &found)) return;
     if (tid == 0) way = wk;
   }
   for (;;) {
@@ -308,11 +310,11 @@ paged_tile(const PagedArgs a) {
     if (tid == 0) {
       Walk<TM, 6> wk = way;
       wk.describe(a, rows, row0);
-      found[0] = wk.next(a);
+      more = wk.next(a);
       way = wk;
     }
     __syncthreads();
-    if (!found[0]) return;
+    if (!more) return;
   }
 }
 

@@ -110,12 +110,21 @@ struct Walk {
   Req<TM, FW> rq;
 
   // Finds the part's beginning; false: the workgroup has none. Every thread of the NT calls it.
+  struct Found {
+    int64_t x;
+    int32_t r;
+    Req<TM, FW> rq;
+  };
   template <int NT>
-  __device__ __forceinline__ bool begin(const PagedArgs& a, int64_t* scan, int64_t* found) {
+  __device__ __forceinline__ bool begin(const PagedArgs& a, int64_t* scan, Found* found) {
     const int tid = threadIdx.x;
     int64_t total = 0, cost = 0, upto = 0;
     auto chunk = [&](int r0, int64_t& sum) __attribute__((always_inline)) {
-      cost = r0 + tid < a.R ? Req<TM, FW>(a, r0 + tid).all(a) * a.Hkv : 0;
+      cost = 0;
+      if (r0 + tid < a.R) {
+        rq = Req<TM, FW>(a, r0 + tid);
+        cost = rq.all(a) * a.Hkv;
+      }
       upto = block_scan<NT>(cost, sum, scan);
       if (tid == NT - 1) scan[0] = upto;
       __syncthreads();
@@ -134,7 +143,7 @@ struct Walk {
     x = cut.start(lw), x1 = cut.start(lw + 1);
     if (x >= x1) return false;
     auto look = [&](int r0) __attribute__((always_inline)) {
-      if (upto - cost <= x && x < upto) found[0] = r0 + tid, found[1] = x - (upto - cost);
+      if (upto - cost <= x && x < upto) *found = Found{x - (upto - cost), r0 + tid, rq};
     };
     if (a.R <= NT) {
       look(0);
@@ -147,9 +156,11 @@ struct Walk {
         __syncthreads();
       }
     }
-    r = uni((int32_t)found[0]);
-    u0 = uni64(found[1]);
-    rq = Req<TM, FW>(a, r);
+    r = uni(found->r);
+    u0 = uni64(found->x);
+    rq = found->rq;
+    rq.first = uni(rq.first), rq.n = uni(rq.n), rq.base = uni(rq.base);
+    rq.rows = uni(rq.rows), rq.tiles = uni(rq.tiles), rq.lastw = uni(rq.lastw);
     const int64_t each = rq.all(a);
     h = (int)(u0 / each);
     u0 -= h * each;
@@ -215,5 +226,5 @@ struct PagedVariant {
   int TM;
   void (*launch)(const lh::PagedArgs& a, hipStream_t st);
 };
-PagedVariant lh_paged_rows_variant(const LhPaged& s, int rows);   // rows a tile: 16 or 32
-PagedVariant lh_paged_tile_variant(const LhPaged& s, int waves);  // waves of 32 rows: 4, 8 or 12 (bf16)
+PagedVariant lh_paged_rows_variant(const LhPaged& s, int64_t rows);  // by the rows of a request
+PagedVariant lh_paged_tile_variant(const LhPaged& s, int waves);    // waves of 32 rows: 4, 8 or 12 (bf16)
