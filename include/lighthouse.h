@@ -329,14 +329,21 @@ lh_status lh_paged_workspace_bytes(const lh_paged* pc, size_t* bytes);
    the requests. A request is admitted whole or not at all: it waits if a length is negative, if it
    would outgrow its table row, if its rows end behind T, or if the pages do not suffice (from the first
    request that lacks pages on, no request that needs one gets any; those that need none go on).
-   Writes the new entries of table; cu_q[r], the sum of the fresh counts before r (clipped at T);
-   kv_len[r] = cached[r] + fresh[r], or 0 for a request that waits; slots[t] and pos[t] of the tokens, -1 where
-   the request waits and behind the last request; n_left[0], what is left of n_free[0]. A page id of
-   free_pages or table outside [0, pages) gives the slot -1. free_pages holds `pages` entries. */
+   Writes
+     - the new entries of table;
+     - cu_q[r], the sum of the fresh counts before r (clipped at T), r = 0 .. R;
+     - kv_len[r] = cached[r] + fresh[r], or 0 for a request that waits;
+     - slots[t] and pos[t] of the tokens, -1 where the request waits and behind the last request;
+     - n_taken[0] (may be NULL), the pages taken: free_pages[0 .. n_free[0] - n_taken[0]) are still free;
+     - balance[0] = n_free[0] less the pages that the requests up to the last admitted one ask for, those that
+       wait for pages among them: what is left, n_free[0] - n_taken[0], unless a request was admitted behind
+       one that waits for pages; then less, and below 0 by the pages that the waiting ones lack.
+   free_pages holds `pages` entries; n_free[0] outside [0, pages] counts as the nearest end. A page
+   id of free_pages or table outside [0, pages) gives the slot -1. */
 lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t* fresh,
                        const int32_t* free_pages, const int32_t* n_free, int32_t* table,
                        int32_t* cu_q, int32_t* kv_len, int32_t* slots, int32_t* pos,
-                       int32_t* n_left, void* stream);
+                       int32_t* balance, int32_t* n_taken, void* stream);
 
 /* Writes K and V rows t into slot slots[t] of the pages, for every t < T. A slot outside
    [0, pages * page) is passed over; every other row of the pages stays as it was. A slot that

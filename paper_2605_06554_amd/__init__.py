@@ -131,7 +131,7 @@ def _load():
         "lh_attention_bwd_indexed": (i32, [PR, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "lh_paged_check": (i32, [PC]),
         "lh_paged_workspace_bytes": (i32, [PC, ctypes.POINTER(sz)]),
-        "lh_page_plan": (i32, [PC, P, P, P, P, P, P, P, P, P, P, P]),
+        "lh_page_plan": (i32, [PC, P, P, P, P, P, P, P, P, P, P, P, P]),
         "lh_page_write": (i32, [PC, P, i64, P, i64, P, P, P, P]),
         "lh_sdpa_paged": (i32, [PC, P, i64, P, P, P, P, P, P, P, P, sz, P]),
     }
@@ -448,14 +448,15 @@ def _xdt(pc):
     return torch.bfloat16 if pc.dtype == LH_BF16 else torch.float32
 
 
-def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, n_left, stream=None):
+def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, balance, n_taken=None, stream=None):
     fn, i32, dev = "lh_page_plan", torch.int32, _device()
     for t, name, n in ((cached, "cached", pc.R), (fresh, "fresh", pc.R), (free_pages, "free_pages", pc.pages),
                        (n_free, "n_free", 1), (table, "table", pc.R * pc.max_blocks), (cu_q, "cu_q", pc.R + 1),
-                       (kv_len, "kv_len", pc.R), (slots, "slots", pc.T), (pos, "pos", pc.T), (n_left, "n_left", 1)):
+                       (kv_len, "kv_len", pc.R), (slots, "slots", pc.T), (pos, "pos", pc.T), (balance, "balance", 1),
+                       (n_taken, "n_taken", 1)):
         _need_on(fn, t, name, i32, n, dev)
     _call(fn, ctypes.byref(pc), _p(cached), _p(fresh), _p(free_pages), _p(n_free), _p(table), _p(cu_q), _p(kv_len),
-          _p(slots), _p(pos), _p(n_left), _stream(stream))
+          _p(slots), _p(pos), _p(balance), _p(n_taken), _stream(stream))
 
 
 def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
@@ -595,10 +596,10 @@ def paged_cache(pages, page, Hkv, D, dtype=torch.bfloat16, device="cuda"):
 
 
 def page_plan(pc, cached, fresh, free_pages, n_free, table, stream=None):
-    """Allocates the outputs and runs lh_page_plan. Returns a dict of cu_q, kv_len, slots, pos and n_left; the new
-    entries of table are written in place."""
+    """Allocates the outputs and runs lh_page_plan. Returns a dict of cu_q, kv_len, slots, pos, balance and n_taken;
+    the new entries of table are written in place. The next step's n_free is this one's less n_taken."""
     e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)  # noqa: E731
-    out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), n_left=e(1))
+    out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), balance=e(1), n_taken=e(1))
     lh_page_plan(pc, cached, fresh, free_pages, n_free, table, *out.values(), stream=stream)
     return out
 

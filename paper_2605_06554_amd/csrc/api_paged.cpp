@@ -85,7 +85,7 @@ lh_status lh_paged_workspace_bytes(const lh_paged* pc, size_t* bytes) {
 
 lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t* fresh, const int32_t* free_pages,
                        const int32_t* n_free, int32_t* table, int32_t* cu_q, int32_t* kv_len, int32_t* slots,
-                       int32_t* pos, int32_t* n_left, void* stream) {
+                       int32_t* pos, int32_t* balance, int32_t* n_taken, void* stream) {
   LhPaged s;
   LH_TRY(make_paged(pc, &s));
   LH_TRY(need(cached, "cached", 4));
@@ -97,10 +97,11 @@ lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t*
   LH_TRY(need(kv_len, "kv_len", 4));
   LH_TRY(need(slots, "slots", 4));
   LH_TRY(need(pos, "pos", 4));
-  LH_TRY(need(n_left, "n_left", 4));
+  LH_TRY(need(balance, "balance", 4));
+  if (n_taken) LH_TRY(need(n_taken, "n_taken", 4));
   lh_fail(LH_OK, "%s", "");
-  return status(lh_launch_page_plan(s, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, n_left,
-                                    (hipStream_t)stream),
+  return status(lh_launch_page_plan(s, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, balance,
+                                    n_taken, (hipStream_t)stream),
                 "lh_page_plan");
 }
 

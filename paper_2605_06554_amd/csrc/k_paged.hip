@@ -11,7 +11,7 @@ __device__ __forceinline__ int64_t blocks_of(int64_t tokens, int shift) {
 
 struct PlanArgs {
   const int32_t *cached, *fresh, *free_pages, *n_free;
-  int32_t *table, *cu_q, *kv_len, *slots, *pos, *n_left;
+  int32_t *table, *cu_q, *kv_len, *slots, *pos, *balance, *n_taken;
   int64_t T, pages;
   int32_t R, max_blocks, shift;
 };
@@ -27,14 +27,14 @@ constexpr int kPlanThreads = 256, kPlanTokens = 4 * kPlanThreads;
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs a) {
   extern __shared__ int32_t lds[];
   __shared__ int64_t part[kPlanThreads / 64];
-  __shared__ int32_t most[kPlanThreads / 64];
+  __shared__ int64_t most[kPlanThreads / 64][2];
   int32_t* const cu = lds;             // [R + 1] first row of every request, clipped at T
   int32_t* const base = lds + a.R + 1;  // [R] pages handed out before the request; -1: it waits
   const int tid = threadIdx.x;
   int64_t n_free = a.n_free[0];
   n_free = n_free < 0 ? 0 : n_free > a.pages ? a.pages : n_free;
   int64_t rows = 0, pages = 0;  // sums up to the last chunk of requests
-  int32_t taken = 0;
+  int64_t taken = 0, asked = 0;  // pages handed out, and asked for by requests up to the last admitted one
   if (tid == 0) cu[0] = 0;
   for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
     const int r = r0 + tid;
@@ -46,7 +46,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
     const int64_t need = fits ? all - blocks_of(c, a.shift) : 0;
     const int64_t upto = block_scan<kPlanThreads>(need, pages, part);
     const bool ok = fits && (need == 0 || upto <= n_free);
-    if (ok && need > 0) taken = (int32_t)upto;  // grows with r
+    if (ok && need > 0) taken = upto;  // (grows with r)
+    if (ok) asked = upto;
     if (real) {
       cu[r + 1] = (int32_t)(end < a.T ? end : a.T);
       base[r] = ok ? (int32_t)(need == 0 ? 0 : upto - need) : -1;
@@ -62,14 +63,19 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
     for (int r = tid; r <= a.R; r += kPlanThreads) a.cu_q[r] = cu[r];
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
-      const int32_t y = __shfl_xor(taken, d, 64);
-      taken = taken > y ? taken : y;
+      const int64_t y = __shfl_xor(taken, d, 64), z = __shfl_xor(asked, d, 64);
+      taken = taken > y ? taken : y, asked = asked > z ? asked : z;
     }
-    if ((tid & 63) == 0) most[tid >> 6] = taken;
+    if ((tid & 63) == 0) most[tid >> 6][0] = taken, most[tid >> 6][1] = asked;
     __syncthreads();
     if (tid == 0) {
-      for (int i = 1; i < kPlanThreads / 64; ++i) taken = taken > most[i] ? taken : most[i];
-      a.n_left[0] = (int32_t)n_free - taken;
+      for (int i = 1; i < kPlanThreads / 64; ++i) {
+        taken = taken > most[i][0] ? taken : most[i][0];
+        asked = asked > most[i][1] ? asked : most[i][1];
+      }
+      const int64_t balance = n_free - asked;
+      a.balance[0] = (int32_t)(balance < INT32_MIN ? INT32_MIN : balance);
+      if (a.n_taken) a.n_taken[0] = (int32_t)taken;
     }
   }
   const int32_t total = cu[a.R];
@@ -138,8 +144,9 @@ using namespace lh;
 
 hipError_t lh_launch_page_plan(const LhPaged& s, const int32_t* cached, const int32_t* fresh,
                                const int32_t* free_pages, const int32_t* n_free, int32_t* table, int32_t* cu_q,
-                               int32_t* kv_len, int32_t* slots, int32_t* pos, int32_t* n_left, hipStream_t st) {
-  const PlanArgs a{cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, n_left,
+                               int32_t* kv_len, int32_t* slots, int32_t* pos, int32_t* balance, int32_t* n_taken,
+                               hipStream_t st) {
+  const PlanArgs a{cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, balance, n_taken,
                    s.T, s.pages, s.R, s.max_blocks, s.shift};
   int64_t blocks = (s.T + kPlanTokens - 1) / kPlanTokens;
   if (blocks > 2048) blocks = 2048;

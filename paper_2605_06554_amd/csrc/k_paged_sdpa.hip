@@ -117,11 +117,17 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a, int TM) {
   }
 }
 
-// The variant that serves a step, by its rows a request (an average: of a step, the host knows only its bounds).
+// The variant that serves a step, by its rows a request (an average: of a step, the host knows only its bounds). Eight
+// requests of 16,000 cached tokens, 32 heads on 8, us, by rows a request: rows kernel (32 a tile), tiles of 128, 256
+// and 384: 16 rows 98 (16 a tile), 106, 119, 127; 48 128, 112, 119, 125; 96 291, 125, 126, 132; 128 201, 134, 130, 137;
+// 256 349, 194, 176, 182; 384 537, 329, 291, 233; 512 664, 346, 306, 348; 1024 1293, 628, 577, 628; one request of
+// 8192 rows 672, 358, 321, 318. Between 256 and 384 the rows that the last tile leaves idle decide.
 static PagedVariant variant_of(const LhPaged& s) {
   const int64_t rows = s.T * s.G / s.R;
-  if (s.dtype == LH_BF16 && rows > 64) return lh_paged_tile_variant(s, rows > 192 ? 12 : 4);
-  return lh_paged_rows_variant(s, rows);
+  if (s.dtype != LH_BF16 || rows <= 32) return lh_paged_rows_variant(s, rows);
+  if (rows <= 112) return lh_paged_tile_variant(s, 4);
+  const int64_t in8 = (rows + 255) / 256 * 256, in12 = (rows + 383) / 384 * 384;
+  return lh_paged_tile_variant(s, rows > 256 && in12 * 32 <= in8 * 33 ? 12 : 8);
 }
 
 template <typename T, int D>

@@ -49,14 +49,14 @@ paged_tile(const PagedArgs a) {
   constexpr int TM = C::TM, FK = C::FK, RB = 2 * D, NT = 64 * NW, LPW = C::LPW;
   __shared__ __align__(16) bf16_t Ks0[FK * D], Ks1[FK * D], Vs0[FK * D], Vs1[FK * D];
   __shared__ int64_t scan[NW];
-  __shared__ typename Walk<TM, 6>::Found found;
+  __shared__ typename Walk<TM, 8>::Found found;
   __shared__ int32_t more;
   const int tid = threadIdx.x, w = uni(tid >> 6);
   // The way along the part waits in LDS while a tile is worked on: in registers (the results of divisions live in
   // vector registers, uniform or not) it made the loop spill 22.
-  __shared__ Walk<TM, 6> way;
+  __shared__ Walk<TM, 8> way;
   {
-    Walk<TM, 6> wk;
+    Walk<TM, 8> wk;
     if (!wk.template begin<NT>(a, scan, &found)) return;
     if (tid == 0) way = wk;
   }
@@ -308,7 +308,7 @@ paged_tile(const PagedArgs a) {
     }
     __syncthreads();  // (the way was read)
     if (tid == 0) {
-      Walk<TM, 6> wk = way;
+      Walk<TM, 8> wk = way;
       wk.describe(a, rows, row0);
       more = wk.next(a);
       way = wk;

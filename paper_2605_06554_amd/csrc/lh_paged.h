@@ -37,7 +37,8 @@ constexpr int32_t kPagedMaxRequests = 4096;
 
 hipError_t lh_launch_page_plan(const LhPaged& s, const int32_t* cached, const int32_t* fresh,
                                const int32_t* free_pages, const int32_t* n_free, int32_t* table, int32_t* cu_q,
-                               int32_t* kv_len, int32_t* slots, int32_t* pos, int32_t* n_left, hipStream_t st);
+                               int32_t* kv_len, int32_t* slots, int32_t* pos, int32_t* balance, int32_t* n_taken,
+                               hipStream_t st);
 hipError_t lh_launch_page_write(const LhPaged& s, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                 const int32_t* slots, void* kpages, void* vpages, hipStream_t st);
 size_t lh_sdpa_paged_ws_bytes(const LhPaged& s);

@@ -49,8 +49,13 @@ inline PagedWs paged_ws(int64_t W, int TM, int D) {
   return w;
 }
 
-constexpr int32_t kOver = 64;    // what a tile costs besides its keys, in keys
-constexpr int32_t kLeast = 256;  // keys below which a part is not worth a workgroup
+constexpr int32_t kCUs = 256;
+template <int TM>
+constexpr int32_t kOver = TM > 128 ? 160 : 64;  // what a tile costs besides its keys, in keys
+// Keys below which a part is not worth a workgroup: with 128 in place of 256, tiles of 16 rows take 11.3 us and not 12.4 (one
+// request, 777 keys) and 16.4 and not 17.7 (4 of 500), larger ones 24 and not 20 (32 rows, 8000 keys).
+template <int TM>
+constexpr int32_t kLeast = TM == 16 ? 128 : 256;
 
 __device__ __forceinline__ int32_t clip(int64_t x, int64_t hi) { return (int32_t)(x < 0 ? 0 : x > hi ? hi : x); }
 __device__ __forceinline__ int32_t uni(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -81,7 +86,7 @@ struct Req {
   }
   // Units of tile t: the keys up to its last row (by whole tokens) and a constant, in 16ths.
   __device__ __forceinline__ int64_t step(const PagedArgs& a) const { return a.G < TM ? TM / a.G : 1; }
-  __device__ __forceinline__ int64_t fixed() const { return (base > 0 ? base : 0) + kOver; }
+  __device__ __forceinline__ int64_t fixed() const { return (base > 0 ? base : 0) + kOver<TM>; }
   __device__ __forceinline__ int64_t units(const PagedArgs& a, int64_t t) const {
     return (fixed() + (t + 1) * step(a)) * (t == tiles - 1 ? lastw : 16);
   }
@@ -132,8 +137,9 @@ struct Walk {
       __syncthreads();
     };
     for (int r0 = 0; r0 < a.R; r0 += NT) chunk(r0, total);
-    const int64_t most = (total + 16 * kLeast - 1) / (16 * kLeast);
-    cut.n = most >= a.W ? a.W : most <= 8 ? 8 : (int32_t)((most + 7) & ~7);
+    const int64_t most = (total + 16 * kLeast<TM> - 1) / (16 * kLeast<TM>);
+    // (between one and two workgroups a CU, those that share one would take twice as long)
+    cut.n = most >= a.W ? a.W : most > kCUs ? kCUs : most <= 8 ? 8 : (int32_t)((most + 7) & ~7);
     cut.q = total / cut.n, cut.rem = total - cut.q * cut.n;
     // neighbouring parts on one XCD (workgroups go to the 8 XCDs in turn): they read the same keys
     const int b = blockIdx.x;

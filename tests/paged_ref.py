@@ -15,9 +15,9 @@ def blocks(tokens, page):
 
 
 def plan(cached, fresh, free_pages, n_free, table, page, pages, T):
-    """Lists in, lists out: (table, cu_q, kv_len, slots, pos, n_left)."""
+    """Lists in, lists out: (table, cu_q, kv_len, slots, pos, pages left, balance)."""
     table, n_free = [list(x) for x in table], min(max(n_free, 0), pages)
-    width, rows, upto, left = len(table[0]), 0, 0, n_free
+    width, rows, upto, left, balance = len(table[0]), 0, 0, n_free, n_free
     cu, kv_len, slots, pos = [0], [], [-1] * T, [-1] * T
     for r, (c, f) in enumerate(zip(cached, fresh)):
         first, rows = rows, rows + max(f, 0)
@@ -28,6 +28,7 @@ def plan(cached, fresh, free_pages, n_free, table, page, pages, T):
         if not ok or (need > 0 and upto > n_free):
             kv_len.append(0)
             continue
+        balance = n_free - upto
         for i in range(need):
             left -= 1
             table[r][blocks(c, page) + i] = free_pages[left]
@@ -37,7 +38,7 @@ def plan(cached, fresh, free_pages, n_free, table, page, pages, T):
             page_id = table[r][p // page]
             pos[first + i] = p
             slots[first + i] = page_id * page + p % page if 0 <= page_id < pages else -1
-    return table, cu, kv_len, slots, pos, left
+    return table, cu, kv_len, slots, pos, left, balance
 
 
 def attend(q, kp, vp, table, cu_q, kv_len, page, scale=0.0, p_half=None):

@@ -50,9 +50,9 @@ def test_plan(R, page, width, T, pages, short):
         tab = _i(table)
         out = lh.page_plan(pc, _i(cached), _i(fresh), _i(free), _i([n_free]), tab)
         ref = paged_ref.plan(cached, fresh, free, n_free, table, page, pages, Tn)
-        for name, got, want in zip(("table", "cu_q", "kv_len", "slots", "pos", "n_left"),
-                                   (tab, out["cu_q"], out["kv_len"], out["slots"], out["pos"], out["n_left"]),
-                                   (*ref[:5], [ref[5]])):
+        for name, got, want in zip(("table", "cu_q", "kv_len", "slots", "pos", "n_taken", "balance"),
+                                   (tab, out["cu_q"], out["kv_len"], out["slots"], out["pos"], out["n_taken"], out["balance"]),
+                                   (*ref[:5], [min(n_free, pages) - ref[5]], [ref[6]])):
             assert torch.equal(got.cpu(), torch.tensor(want, dtype=I32)), name
 
 
@@ -69,7 +69,7 @@ def test_plan_of_bad_pages_and_counts():
         ref = paged_ref.plan(*args, table, 16, 8, 64)
         for got, want in zip((tab, out["cu_q"], out["kv_len"], out["slots"], out["pos"]), ref):
             assert torch.equal(got.cpu(), torch.tensor(want, dtype=I32))
-        assert int(out["n_left"]) == ref[5]
+        assert int(out["n_taken"]) == min(max(n_free, 0), 8) - ref[5] and int(out["balance"]) == ref[6]
 
 
 def test_plan_of_large_lengths():
@@ -352,7 +352,7 @@ def test_pool_beyond_32_bit_offsets():
 def _serve(pc, state, q, k, v, cached, fresh, ws):
     plan = lh.page_plan(pc, _i(cached), _i(fresh), state["free"], state["n_free"], state["table"])
     o, lse = lh.attention_paged(pc, q, k, v, state["kp"], state["vp"], state["table"], plan, ws)
-    state["n_free"] = plan["n_left"]
+    state["n_free"] = state["n_free"] - plan["n_taken"]
     return plan, o, lse
 
 

@@ -46,9 +46,10 @@ def test_null_and_misaligned_pointers():
     for i in range(10):  # each pointer of the plan in turn
         bad = ok[:10]
         bad[i] = None
-        assert lib.lh_page_plan(by, *bad, None) == -1
+        assert lib.lh_page_plan(by, *bad, ok[10], None) == -1
         bad[i] = 0x10002
-        assert lib.lh_page_plan(by, *bad, None) == -5
+        assert lib.lh_page_plan(by, *bad, None, None) == -5
+    assert lib.lh_page_plan(by, *ok[:10], 0x10001, None) == -5
     row = 2 * 64
     for args, code in [((None, row, 0x1000, row, 0x2000, 0x3000, 0x4000), -1),
                        ((0x1008, row, 0x1000, row, 0x2000, 0x3000, 0x4000), -5),
@@ -144,9 +145,9 @@ def test_reference_plan_hands_out_pages_in_order():
     request 1 brings nothing; request 2 lacks pages and waits; request 3 needs none and goes on; request 4 waits."""
     table = [[7, -1, -1], [3, -1, -1], [-1] * 3, [5, -1, -1], [-1] * 3]
     got = paged_ref.plan([10, 16, 0, 1, 0], [8, 0, 33, 2, 1], [20, 21, 22, 99], 3, table, 16, 64, 44)
-    t, cu, kv, slots, pos, left = got
+    t, cu, kv, slots, pos, left, balance = got
     assert t == [[7, 22, -1], [3, -1, -1], [-1] * 3, [5, -1, -1], [-1] * 3]
-    assert cu == [0, 8, 8, 41, 43, 44] and kv == [18, 16, 0, 3, 0] and left == 2
+    assert cu == [0, 8, 8, 41, 43, 44] and kv == [18, 16, 0, 3, 0] and left == 2 and balance == 3 - 4
     assert slots[:8] == [7 * 16 + x for x in range(10, 16)] + [22 * 16, 22 * 16 + 1]
     assert slots[8:41] == [-1] * 33 and slots[41:] == [81, 82, -1] and pos[41:] == [1, 2, -1]
 
