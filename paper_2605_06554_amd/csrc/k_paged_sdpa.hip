@@ -8,113 +8,105 @@
 
 namespace lh {
 
-// Joins the parts of the tiles that were cut: a workgroup to 16 rows of a tile, 16 lanes to a row, all parts of a row in
-// flight at once where they are 8 at most; longer chains are shared by four groups of lanes, whose sums
-// are added in order. Small tiles (of the rows kernel) take four groups a row and a workgroup to 4 rows.
-// Bound by the latency of three dependent loads (which tile, its statistics, its rows), and by HBM where tiles
-// are large.
-constexpr int kJoinFew = 8;
-__host__ __device__ __forceinline__ constexpr int join_rows(int TM) { return TM > 32 ? 16 : 4; }  // a workgroup
+// Joins the parts of the tiles that were cut: 16 lanes to a row and group of parts, which reads its parts FEW at a time,
+// all in flight at once, with a running maximum; S groups share the parts of a row and are joined in LDS, in order.
+// Small tiles (of the rows kernel) take S = 4 and a workgroup to 4 rows, large ones S = 1 and 16 rows. Bound by the
+// latency of two dependent loads (which tile, its parts) and the launch, and by HBM where tiles are large.
+template <bool SMALL>
+struct JoinCfg {
+  static constexpr int S = SMALL ? 4 : 1, FEW = SMALL ? 4 : 8, ROWS = 16 / S;
+};
 
-template <typename T, int D>
+template <typename T, int D, bool SMALL>
 __global__ void __launch_bounds__(256) paged_join(const PagedArgs a, int TM) {
+  using C = JoinCfg<SMALL>;
   constexpr int E = D / 16;  // columns a lane
-  __shared__ __align__(16) float acc_s[16][D];
-  __shared__ float l_s[16];
-  const int lw = blockIdx.x, per = join_rows(TM), y0 = blockIdx.y * per;
+  __shared__ __align__(16) float acc_s[SMALL ? 16 : 1][D];
+  __shared__ float m_s[16], l_s[16];
+  const int lw = blockIdx.x, y0 = blockIdx.y * C::ROWS;
   const PartDesc d = a.desc[lw];
   if (y0 >= d.rows) return;
   const int count = uni(d.last) - lw + 1, grp = threadIdx.x >> 4, c = (threadIdx.x & 15) * E;
-  const int S = per == 4 || count > kJoinFew ? 4 : 1;  // groups a row
-  for (int pass = 0; pass < per * S / 16 && y0 + pass * (16 / S) < d.rows; ++pass) {
-    const int row = y0 + pass * (16 / S) + grp / S, sub = grp % S;
-    const bool real = row < d.rows;
-    float acc[E], l = 0.0f, mt = -INFINITY;
+  const int row = y0 + grp / C::S, sub = grp % C::S;
+  const bool real = row < d.rows;
+  float acc[E], l = 0.0f, m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  // A part with the maximum -inf has no weights: its sum is 0, or NaN where all its logits are.
+  auto weight = [&](float x, float top) __attribute__((always_inline)) { return x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(x - top); };
+  if (real) {
+    for (int p0 = sub; p0 < count; p0 += C::S * C::FEW) {
+      float2 st[C::FEW];
+      float4 x[C::FEW][E / 4];
+#pragma unroll
+      for (int i = 0; i < C::FEW; ++i) {
+        const int p = p0 + C::S * i;
+        st[i] = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int z = 0; z < E / 4; ++z) x[i][z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (p < count) {
+          const int64_t at = (2 * (int64_t)(lw + p) + (p == 0 ? 1 : 0)) * TM + row;
+          st[i] = a.stat[at];
+#pragma unroll
+          for (int z = 0; z < E / 4; ++z) x[i][z] = *reinterpret_cast<const float4*>(a.part + at * D + c + 4 * z);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int i = 0; i < C::FEW; ++i) top = fmaxf(top, st[i].x);
+      const float al = weight(m, top);
+      m = top, l *= al;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] *= al;
+#pragma unroll
+      for (int i = 0; i < C::FEW; ++i) {
+        const float wt = weight(st[i].x, top);
+        l += wt * st[i].y;
+#pragma unroll
+        for (int z = 0; z < E / 4; ++z) {
+          acc[4 * z] += wt * x[i][z].x, acc[4 * z + 1] += wt * x[i][z].y;
+          acc[4 * z + 2] += wt * x[i][z].z, acc[4 * z + 3] += wt * x[i][z].w;
+        }
+      }
+    }
+  }
+  if constexpr (SMALL) {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(&acc_s[grp][c + e]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+    if (c == 0) m_s[grp] = m, l_s[grp] = l;
+    __syncthreads();
+    if (sub != 0) return;
+#pragma unroll
+    for (int z = 1; z < 4; ++z) m = fmaxf(m, m_s[grp + z]);
+    l = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-    if (real) {
-      auto slot = [&](int p) __attribute__((always_inline)) { return (2 * (int64_t)(lw + p) + (p == 0 ? 1 : 0)) * TM + row; };
-      auto add = [&](float2 st, const float4* x) __attribute__((always_inline)) {
-        const float wt = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - mt);
-        l += st.x == -INFINITY ? st.y : wt * st.y;  // (the sum of a part whose logits are all NaN is NaN)
 #pragma unroll
-        for (int z = 0; z < E / 4; ++z)
-          acc[4 * z] += wt * x[z].x, acc[4 * z + 1] += wt * x[z].y, acc[4 * z + 2] += wt * x[z].z, acc[4 * z + 3] += wt * x[z].w;
-      };
-      if (S == 1) {
-        float2 st[kJoinFew];
-        float4 x[kJoinFew][E / 4];
+    for (int z = 0; z < 4; ++z) {
+      const float wt = weight(m_s[grp + z], m);
+      l += wt * l_s[grp + z];
 #pragma unroll
-        for (int p = 0; p < kJoinFew; ++p) {
-          st[p] = make_float2(-INFINITY, 0.0f);
-#pragma unroll
-          for (int z = 0; z < E / 4; ++z) x[p][z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          if (p < count) {
-            st[p] = a.stat[slot(p)];
-#pragma unroll
-            for (int z = 0; z < E / 4; ++z) x[p][z] = *reinterpret_cast<const float4*>(a.part + slot(p) * D + c + 4 * z);
-          }
-        }
-#pragma unroll
-        for (int p = 0; p < kJoinFew; ++p) mt = fmaxf(mt, st[p].x);
-#pragma unroll
-        for (int p = 0; p < kJoinFew; ++p) add(st[p], x[p]);
-      } else {
-        for (int p = threadIdx.x & 15; p < count; p += 16) mt = fmaxf(mt, a.stat[slot(p)].x);
-#pragma unroll
-        for (int z = 8; z > 0; z >>= 1) mt = fmaxf(mt, __shfl_xor(mt, z, 64));
-        for (int p0 = sub; p0 < count; p0 += 4 * kJoinFew) {
-          float2 st[kJoinFew];
-          float4 x[kJoinFew][E / 4];
-#pragma unroll
-          for (int i = 0; i < kJoinFew; ++i) {
-            const int p = p0 + 4 * i < count ? p0 + 4 * i : p0;  // (a part past the last is read and not added)
-            st[i] = a.stat[slot(p)];
-#pragma unroll
-            for (int z = 0; z < E / 4; ++z) x[i][z] = *reinterpret_cast<const float4*>(a.part + slot(p) * D + c + 4 * z);
-          }
-#pragma unroll
-          for (int i = 0; i < kJoinFew; ++i)
-            if (p0 + 4 * i < count) add(st[i], x[i]);
-        }
-      }
+      for (int e = 0; e < E; ++e) acc[e] += wt * acc_s[grp + z][c + e];
     }
-    if (S > 1) {
-#pragma unroll
-      for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(&acc_s[grp][c + e]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-      if (c == 0) l_s[grp] = l;
-      __syncthreads();
-      l = 0.0f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        l += l_s[(grp & ~3) + z];
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += acc_s[(grp & ~3) + z][c + e];
-      }
-      __syncthreads();
-      if (sub != 0) continue;
-    }
-    if (!real) continue;
-    const int gr = d.row0 + row, tok = gr / a.G;
-    const int64_t at = (int64_t)(d.first + tok) * a.Hq + d.head * a.G + (gr - tok * a.G);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] *= inv;
-    T* const o = (T*)a.o + at * D + c;
-    if constexpr (sizeof(T) == 4) {
-#pragma unroll
-      for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(o + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-    } else {
-      uint32_t y[E / 2];
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) y[e] = (uint32_t)f2bf(acc[2 * e]) | ((uint32_t)f2bf(acc[2 * e + 1]) << 16);
-      if constexpr (E == 8) *reinterpret_cast<uint4*>(o) = make_uint4(y[0], y[1], y[2], y[3]);
-      else *reinterpret_cast<uint2*>(o) = make_uint2(y[0], y[1]);
-    }
-    if (a.lse && c == 0) a.lse[at] = l == 0.0f ? -INFINITY : (mt + __log2f(l)) * kLn2;
   }
+  if (!real) return;
+  const int gr = d.row0 + row, tok = gr / a.G;
+  const int64_t at = (int64_t)(d.first + tok) * a.Hq + d.head * a.G + (gr - tok * a.G);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] *= inv;
+  T* const o = (T*)a.o + at * D + c;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(o + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+  } else {
+    uint32_t y[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) y[e] = (uint32_t)f2bf(acc[2 * e]) | ((uint32_t)f2bf(acc[2 * e + 1]) << 16);
+    if constexpr (E == 8) *reinterpret_cast<uint4*>(o) = make_uint4(y[0], y[1], y[2], y[3]);
+    else *reinterpret_cast<uint2*>(o) = make_uint2(y[0], y[1]);
+  }
+  if (a.lse && c == 0) a.lse[at] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
 }
 
 // The variant that serves a step, by its rows a request (an average: of a step, the host knows only its bounds). Eight
@@ -130,10 +122,15 @@ static PagedVariant variant_of(const LhPaged& s) {
   return lh_paged_tile_variant(s, rows > 256 && in12 * 32 <= in8 * 33 ? 12 : 8);
 }
 
+template <typename T, int D, bool SMALL>
+static void launch_join(const LhPaged& s, const PagedArgs& a, int TM, hipStream_t st) {
+  const int64_t rows = s.T * s.G < TM ? s.T * s.G : TM, per = JoinCfg<SMALL>::ROWS;
+  hipLaunchKernelGGL((paged_join<T, D, SMALL>), dim3((unsigned)a.W, (unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a, TM);
+}
 template <typename T, int D>
 static void launch_join(const LhPaged& s, const PagedArgs& a, int TM, hipStream_t st) {
-  const int64_t rows = s.T * s.G < TM ? s.T * s.G : TM;
-  hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)a.W, (unsigned)((rows + join_rows(TM) - 1) / join_rows(TM))), dim3(256), 0, st, a, TM);
+  if (sizeof(T) == 4 || TM <= 32) launch_join<T, D, true>(s, a, TM, st);
+  else if constexpr (sizeof(T) == 2) launch_join<T, D, false>(s, a, TM, st);
 }
 
 }  // namespace lh
