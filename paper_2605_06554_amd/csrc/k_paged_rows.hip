@@ -1,383 +1,55 @@
-// k_paged_rows.hip -- attention over a paged cache, for requests of few rows (decoding, drafts) and for
-// fp32 (rows, cut and parts: lh_paged_sdpa.h). Tiles of 16 or 32 rows: with one new token a tile has G
-// rows, the product with them costs a 16-row MFMA whatever G is, and the kernel is bound by the bytes of
-// K and V.
-//
-// Within a part, the four waves take its blocks of keys in turn, each with a running maximum and sum of its own,
-// and are joined in LDS at the end of the tile.
-//
-// Registers only. A wave's loop uses no LDS and no barrier:
-//   bf16, MFMA 16x16x32, lane l, n = l % 16, g = l / 16: A[m = n][k = 8 g + 0..7], B[k = 8 g + 0..7][n],
-//   C[m = 4 g + i][n], i = 0..3.
-//   S^T = K Q^T: a lane reads 16 bytes of key n of 16 keys (64 consecutive bytes a row and load).
-//   O^T = V^T P^T: the k order is the keys 4 g + 0..3 and 16 + 4 g + 0..3 of a 32-key block, the order
-//   in which the lane holds S^T, so P is the operand as it is computed. V^T's operand is 8 keys of one column;
-//   a lane reads D / 16 consecutive columns of those 8 keys (whole rows a wave) and transposes
-//   them in registers, one v_perm_b32 for two values; its columns are d = (D / 16) m + s of MFMA s, which
-//   permutes the columns of O^T and not the sums, and hands a lane consecutive columns to store.
-//   fp32, MFMA 16x16x4: A[m = n][k = g] one value; the k order of step c of 4 is column 16 kk + 4 g + c (a
-//   16-byte read), and of V step i the key 4 g + i, whose columns need no transpose at all.
-// The loads of the next block's K are issued when the last ones were multiplied, the same for V; 8 waves a CU keep
-// enough of them in flight (64 requests, 482,000 keys: 312 us with 8 waves, 325 with 12, 327 with 4).
-#include <math.h>
-
-#include "lh_mfma.h"
-#include "lh_paged_sdpa.h"
+// k_paged_rows.hip -- attention over a paged cache for requests of few rows (decoding, drafts) and for fp32: tiles
+// of 16 or 32 rows (lh_paged_rows.h), workgroups of four waves, two of them a CU: 8 waves keep enough loads in
+// flight (64 requests, 482,000 keys: 312 us with 8 waves a CU, 325 with 12, 327 with 4), and workgroups of their own
+// keep loading while one joins its waves (12 waves in one workgroup: 372 us where four took 352).
+#include "lh_paged_rows.h"
 
 namespace lh {
 
-typedef __attribute__((__vector_size__(4 * sizeof(uint32_t)))) uint32_t u32v4;
-typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32v2;
+constexpr int kRowsNW = 4, kRowsEU = 2;  // waves, and workgroups a CU
+constexpr int64_t kRowsW = kCUs * kRowsEU;
 
-template <typename T, int D, int RT>
-struct RowsCfg {
-  static constexpr int NW = 4, TM = 16 * RT, KB = sizeof(T) == 2 ? 32 : 16;  // keys of a block
-  static constexpr int DL = D / 16;                                           // columns of V that a lane reads
-  static constexpr int KV = KB / 16 * D / (sizeof(T) == 2 ? 32 : 16);         // 16-byte reads of K a lane and block
-  static constexpr int NV = KB / 4;                                           // keys of V a lane and block
-  static constexpr int VW = DL * sizeof(T) / 4;                               // 32-bit words of one of them
-  static constexpr int EU = 2;  // workgroups a CU
-  static constexpr int64_t W = 256 * EU;
-};
-
-template <bool NT, typename V>
-__device__ __forceinline__ V load(const char* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
-  else return *reinterpret_cast<const V*>(p);
-}
-
-template <typename T, int D, int RT>
-struct Wave {
-  using C = RowsCfg<T, D, RT>;
-  f32x4 acc[RT][C::DL];
-  float m[RT], l[RT];  // of row n; the sum is this lane's share
-  u32v4 q[RT][D * sizeof(T) / 64];
-  u32v4 k[C::KV];
-  uint32_t v[C::NV][C::VW];
+template <int D>
+struct RowsLds {
+  static constexpr int PER = kRowsNW;
+  float (*parts)[16 * D], (*stat)[16];
+  __device__ __forceinline__ float* part(int w) const { return parts[w]; }
+  __device__ __forceinline__ float* words(int w) const { return parts[w]; }
+  __device__ __forceinline__ float* ms(int w) const { return stat[w]; }
+  __device__ __forceinline__ float* ls(int w) const { return stat[kRowsNW + w]; }
 };
 
 // NT: K and V are loaded with the non-temporal hint.
 template <typename T, int D, int RT, bool NT>
-__global__ void __launch_bounds__(256, (RowsCfg<T, D, RT>::EU)) paged_rows(const PagedArgs a) {
-  using C = RowsCfg<T, D, RT>;
-  constexpr int TM = C::TM, DL = C::DL, KB = C::KB, RB = D * (int)sizeof(T);
-  constexpr bool B16 = sizeof(T) == 2;
-  constexpr int LD = D + 4;  // a row of the LDS parts, padded by 16 bytes
-  __shared__ __align__(16) float parts[C::NW][16][LD];
-  __shared__ float ms[C::NW][16], ls[C::NW][16];
-  __shared__ int64_t scan[C::NW];
+__global__ void __launch_bounds__(64 * kRowsNW, kRowsEU) paged_rows(const PagedArgs a) {
+  constexpr int TM = 16 * RT, KB = RowsCfg<T, D, RT>::KB;
+  __shared__ __align__(16) float parts[kRowsNW][16 * D];
+  __shared__ float stat[2 * kRowsNW][16];
+  __shared__ int64_t scan[kRowsNW];
   __shared__ typename Walk<TM, 16>::Found found;
-  const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6), n = lane & 15, g = lane >> 4;
-
   Walk<TM, 16> wk;
-  if (!wk.template begin<256>(a, scan, &found)) return;
-  Wave<T, D, RT> s;
+  if (!wk.template begin<64 * kRowsNW>(a, scan, &found)) return;
   do {
-    const int first = uni(wk.rq.first), base = uni(wk.rq.base), all_rows = uni(wk.rq.rows);
-    const int r = uni(wk.r), h = uni(wk.h), row0 = uni(wk.t) * TM, rows = all_rows - row0 < TM ? all_rows - row0 : TM;
-    const int keys = uni(base + (row0 + rows - 1) / a.G + 1);  // that any row of the tile sees
-    const int safe = uni(base + row0 / a.G + 1);               // that all of them see
+    RowsItem it;
+    it.first = uni(wk.rq.first), it.base = uni(wk.rq.base), it.all_rows = uni(wk.rq.rows);
+    it.r = uni(wk.r), it.h = uni(wk.h), it.row0 = uni(wk.t) * TM;
+    it.rows = it.all_rows - it.row0 < TM ? it.all_rows - it.row0 : TM;
+    it.keys = uni(it.base + (it.row0 + it.rows - 1) / a.G + 1);
+    it.safe = uni(it.base + it.row0 / a.G + 1);
     int b0, b1;
-    wk.blocks(keys > 0 ? (keys + KB - 1) / KB : 0, b0, b1);
-    b0 = uni(b0), b1 = uni(b1);
-
-    // ---- this wave's blocks
-    int pos[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      int row = row0 + rt * 16 + n;
-      row = row < all_rows ? row : all_rows - 1;
-      const int tok = row / a.G;
-      pos[rt] = base + tok;
-      const T* qp = (const T*)a.q + (int64_t)(first + tok) * a.q_stride + (int64_t)(h * a.G + row - tok * a.G) * D;
-#pragma unroll
-      for (int c = 0; c < RB / 64; ++c) s.q[rt][c] = *reinterpret_cast<const u32v4*>((const char*)qp + c * 64 + g * 16);
-      s.m[rt] = -INFINITY, s.l[rt] = 0.0f;
-#pragma unroll
-      for (int e = 0; e < DL; ++e) s.acc[rt][e] = f32x4{};
-    }
-    const int64_t ids = (int64_t)r * a.max_blocks;  // the request's row of the table
-    const int last = (keys - 1) >> a.shift;  // the last page in use (keys > 0 wherever it is used)
-    // A block's pages are looked up a block ahead of its loads; K and V lie at the same place of their pools.
-    int32_t pg[KB / 16];
-    int64_t off[KB / 16];  // bytes from the pool's start to 16 keys
-    auto look_up = [&](int j) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < KB / 16; ++c) {
-        const int b = (j + 16 * c) >> a.shift;
-        pg[c] = page_id(a.table, ids + (b < last ? b : last), a.pages);
-      }
-    };
-    auto place = [&](int j) __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < KB / 16; ++c)
-        off[c] = ((((int64_t)pg[c] * a.Hkv + h) << a.shift) + ((j + 16 * c) & ((1 << a.shift) - 1))) * RB;
-    };
-    auto load_k = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < KB / 16; ++c) {
-        const char* p = (const char*)a.kp + off[c];
-#pragma unroll
-        for (int i = 0; i < RB / 64; ++i)
-          s.k[c * (RB / 64) + i] = load<NT, u32v4>(p + n * RB + g * 16 + i * 64);
-      }
-    };
-    auto load_v = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int c = 0; c < KB / 16; ++c) {
-        const char* p = (const char*)a.vp + off[c];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const char* pv = p + (4 * g + i) * RB + n * (DL * (int)sizeof(T));
-          if constexpr (C::VW == 2) {
-            const u32v2 y = load<NT, u32v2>(pv);
-            s.v[4 * c + i][0] = y[0], s.v[4 * c + i][1] = y[1];
-          } else {
-#pragma unroll
-            for (int z = 0; z < C::VW / 4; ++z) {
-              const u32v4 y = load<NT, u32v4>(pv + 16 * z);
-#pragma unroll
-              for (int o = 0; o < 4; ++o) s.v[4 * c + i][4 * z + o] = y[o];
-            }
-          }
-        }
-      }
-    };
-    // O^T += V^T P^T; p[rt]: this lane's weights of its keys
-    auto pv = [&](const float (*p)[C::NV]) __attribute__((always_inline)) {
-      if constexpr (B16) {
-        bf16x8 pb[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) pb[rt] = cvt8(p[rt]);  // one rounding, to the type of V
-#pragma unroll
-        for (int e = 0; e < DL; ++e) {
-          u32v4 y;
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            y[c] = __builtin_amdgcn_perm(s.v[2 * c + 1][e / 2], s.v[2 * c][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            s.acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y), pb[rt], s.acc[rt][e], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < DL; ++e)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-              s.acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(s.v[i][e]), p[rt][i], s.acc[rt][e], 0, 0, 0);
-      }
-    };
-    // Takes the values of V that are not finite out of the registers and adds them to the rows that see their
-    // key. (They may be of keys that some rows see and others do not, and 0 times them would be NaN.) A product
-    // with the rows' view of the keys (1 or 0) counts them, 1 for +inf, 64 for -inf, 4096 for NaN: of
-    // at most 32 keys, so the counts do not overlap. A rare path that must not cost the loop registers: the
-    // words go through the wave's part of the LDS, and the columns are a loop that is not unrolled.
-    auto odd_values = [&](int j0) __attribute__((always_inline)) {
-      uint32_t* const mine = reinterpret_cast<uint32_t*>(&parts[w][0][0]) + lane;
-      static_assert(C::NV * C::VW * 64 <= 16 * LD, "the words of a block fit a wave's part");
-#pragma unroll
-      for (int i = 0; i < C::NV; ++i)
-#pragma unroll
-        for (int z = 0; z < C::VW; ++z) {
-          uint32_t& y = s.v[i][z];
-          mine[(i * C::VW + z) * 64] = y;
-          if constexpr (B16) {
-            if ((y & 0x7f80u) == 0x7f80u) y &= 0xffff0000u;
-            if ((y & 0x7f800000u) == 0x7f800000u) y &= 0x0000ffffu;
-          } else {
-            if ((y & 0x7f800000u) == 0x7f800000u) y = 0;
-          }
-        }
-#pragma unroll 1
-      for (int e = 0; e < DL; ++e) {
-        float code[C::NV], see[C::NV];
-#pragma unroll
-        for (int i = 0; i < C::NV; ++i) {
-          const uint32_t y = mine[(i * C::VW + (B16 ? e / 2 : e)) * 64];
-          const uint32_t x = B16 ? (e & 1 ? y & 0xffff0000u : y << 16) : y;
-          code[i] = (x & 0x7f800000u) != 0x7f800000u ? 0.0f : x & 0x7fffffu ? 4096.0f : x >> 31 ? 64.0f : 1.0f;
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-          for (int i = 0; i < C::NV; ++i) see[i] = j0 + 16 * (i / 4) + 4 * g + i % 4 <= pos[rt] ? 1.0f : 0.0f;
-          f32x4 cnt = {};
-          if constexpr (B16) {
-            cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cvt8(code), cvt8(see), cnt, 0, 0, 0);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) cnt = __builtin_amdgcn_mfma_f32_16x16x4f32(code[i], see[i], cnt, 0, 0, 0);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int c = (int)cnt[i];
-            const float add = c == 0 ? 0.0f : c >> 12 || ((c & 63) && (c >> 6)) ? NAN : c & 63 ? INFINITY : -INFINITY;
-#pragma unroll
-            for (int y = 0; y < DL; ++y) s.acc[rt][y][i] += y == e ? add : 0.0f;
-          }
-        }
-      }
-    };
-    int blk = b0 + w;
-    if (blk < b1) {
-      look_up(blk * KB);
-      place(blk * KB);
-      load_k();
-      load_v();
-      look_up((blk + C::NW) * KB);
-    }
-    for (; blk < b1; blk += C::NW) {
-      const int j0 = blk * KB, next = (blk + C::NW) * KB;
-      const bool more = blk + C::NW < b1;
-      f32x4 sc[RT][KB / 16];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int c = 0; c < KB / 16; ++c) {
-          sc[rt][c] = f32x4{};
-#pragma unroll
-          for (int i = 0; i < RB / 64; ++i) {
-            const u32v4 kk = s.k[c * (RB / 64) + i], qq = s.q[rt][i];
-            if constexpr (B16) {
-              sc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, qq),
-                                                                   sc[rt][c], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int o = 0; o < 4; ++o)
-                sc[rt][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kk[o]), __uint_as_float(qq[o]), sc[rt][c], 0, 0, 0);
-            }
-          }
-        }
-      if (more) {
-        place(next);
-        load_k();
-        look_up(next + C::NW * KB);
-      }
-      const bool masked = j0 + KB > safe;
-      if (masked) {
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int c = 0; c < KB / 16; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (j0 + 16 * c + 4 * g + i > pos[rt]) sc[rt][c][i] = -INFINITY;
-      }
-      float p[RT][C::NV];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float top = sc[rt][0][0];
-#pragma unroll
-        for (int c = 0; c < KB / 16; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][c][i]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64)) * a.sl2;
-        const bool grown = top > s.m[rt] + kRescale;  // each row by its own: no row's bits depend on another's
-        if (__any(grown)) {
-          const float al = !grown ? 1.0f : s.m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s.m[rt] - top);
-          s.m[rt] = grown ? top : s.m[rt], s.l[rt] *= al;
-#pragma unroll
-          for (int e = 0; e < DL; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.acc[rt][e][i] *= al;
-        }
-        const float mm = s.m[rt] == -INFINITY ? 0.0f : s.m[rt];  // no key yet: all weights are 0
-#pragma unroll
-        for (int c = 0; c < KB / 16; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[rt][4 * c + i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][c][i], a.sl2, -mm));
-            s.l[rt] += p[rt][4 * c + i];
-          }
-      }
-      bool odd = false;
-      if (masked) {  // rows behind the last key hold anything: they count as 0
-#pragma unroll
-        for (int i = 0; i < C::NV; ++i) {
-          const bool in = j0 + 16 * (i / 4) + 4 * g + i % 4 < keys;
-#pragma unroll
-          for (int z = 0; z < C::VW; ++z) {
-            uint32_t& y = s.v[i][z];
-            y = in ? y : 0u;
-            odd |= (y & 0x7f800000u) == 0x7f800000u || (B16 && (y & 0x7f80u) == 0x7f80u);
-          }
-        }
-      }
-      if (__any(odd)) odd_values(j0);
-      pv(p);
-      if (more) load_v();
-    }
-
-    // ---- the four waves joined
-    const bool whole = wk.whole();
-    const int64_t slot = wk.slot();
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float l = s.l[rt];
-      l += __shfl_xor(l, 16, 64);
-      l += __shfl_xor(l, 32, 64);
-      if (g == 0) ms[w][n] = s.m[rt], ls[w][n] = l;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < DL; e += 4)
-          *reinterpret_cast<f32x4*>(&parts[w][n][DL * (4 * g + i) + e]) =
-              f32x4{s.acc[rt][e][i], s.acc[rt][e + 1][i], s.acc[rt][e + 2][i], s.acc[rt][e + 3][i]};
-      __syncthreads();
-      const int rn = tid >> 4, c0 = (tid & 15) * DL, row = rt * 16 + rn;
-      if (row < rows) {
-        float mt = ms[0][rn], lt = 0.0f, out[DL];
-#pragma unroll
-        for (int y = 1; y < C::NW; ++y) mt = fmaxf(mt, ms[y][rn]);
-#pragma unroll
-        for (int e = 0; e < DL; ++e) out[e] = 0.0f;
-#pragma unroll
-        for (int y = 0; y < C::NW; ++y) {
-          const float wt = ms[y][rn] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ms[y][rn] - mt);
-          if (ms[y][rn] != -INFINITY || ls[y][rn] != 0.0f) {  // (a NaN sum comes with a maximum of -inf where all logits are NaN)
-            lt += ms[y][rn] == -INFINITY ? ls[y][rn] : wt * ls[y][rn];
-#pragma unroll
-            for (int e = 0; e < DL; ++e) out[e] += wt * parts[y][rn][c0 + e];
-          }
-        }
-        if (whole) {
-          const int gr = row0 + row, tok = gr / a.G;
-          const int64_t at_ = (int64_t)(first + tok) * a.Hq + h * a.G + (gr - tok * a.G);
-          const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-          T* o = (T*)a.o + at_ * D + c0;
-          if constexpr (B16) {
-            uint32_t y[DL / 2];
-#pragma unroll
-            for (int e = 0; e < DL / 2; ++e) y[e] = (uint32_t)f2bf(out[2 * e] * inv) | ((uint32_t)f2bf(out[2 * e + 1] * inv) << 16);
-            if constexpr (DL == 8) *reinterpret_cast<u32v4*>(o) = u32v4{y[0], y[1], y[2], y[3]};
-            else *reinterpret_cast<u32v2*>(o) = u32v2{y[0], y[1]};
-          } else {
-#pragma unroll
-            for (int e = 0; e < DL; e += 4)
-              *reinterpret_cast<f32x4*>(o + e) = f32x4{out[e] * inv, out[e + 1] * inv, out[e + 2] * inv, out[e + 3] * inv};
-          }
-          if (a.lse && (tid & 15) == 0) a.lse[at_] = lt == 0.0f ? -INFINITY : (mt + __log2f(lt)) * kLn2;
-        } else {
-          float* o = a.part + (slot * TM + row) * D + c0;
-#pragma unroll
-          for (int e = 0; e < DL; e += 4) *reinterpret_cast<f32x4*>(o + e) = f32x4{out[e], out[e + 1], out[e + 2], out[e + 3]};
-          if ((tid & 15) == 0) a.stat[slot * TM + row] = make_float2(mt, lt);
-        }
-      }
-      __syncthreads();
-    }
-    if (tid == 0) wk.describe(a, rows, row0);
+    wk.blocks(it.keys > 0 ? (it.keys + KB - 1) / KB : 0, b0, b1);
+    it.b0 = uni(b0), it.b1 = uni(b1);
+    it.whole = wk.whole(), it.slot = wk.slot();
+    rows_tile<T, D, RT, kRowsNW, NT, TM>(a, it, RowsLds<D>{parts, stat});
+    if (threadIdx.x == 0) wk.describe(a, it.rows, it.row0);
+    __syncthreads();  // the parts were read
   } while (wk.next(a));
 }
 
 template <typename T, int D, int RT, bool NT>
 static PagedVariant variant() {
-  using C = RowsCfg<T, D, RT>;
-  return {C::W, C::TM, [](const PagedArgs& a, hipStream_t st) {
-            hipLaunchKernelGGL((paged_rows<T, D, RT, NT>), dim3((unsigned)C::W), dim3(256), 0, st, a);
+  return {kRowsW, 16 * RT, [](const PagedArgs& a, hipStream_t st) {
+            hipLaunchKernelGGL((paged_rows<T, D, RT, NT>), dim3((unsigned)kRowsW), dim3(256), 0, st, a);
           }};
 }
 // A request of one tile reads its keys once, and the non-temporal hint is worth 8% of the time (6.1 against 5.6

@@ -71,8 +71,8 @@ __device__ __forceinline__ int32_t page_id(const int32_t* table, int64_t i, int6
 }
 
 // What a request asks for. Lengths and offsets are clipped into their ranges. FW: what a key costs a tile
-// whatever its rows, in 16ths of what it costs a full one.
-template <int TM, int FW>
+// whatever its rows, in 16ths of what it costs a full one; NR: what it costs 16 rows or fewer, if that differs.
+template <int TM, int FW, int NR>
 struct Req {
   int32_t first, n, base, rows, tiles, lastw;  // base: position of the first new token
   __device__ __forceinline__ Req() {}
@@ -82,16 +82,17 @@ struct Req {
     base = clip(a.kv_len[r], (int64_t)a.max_blocks << a.shift) - n;
     rows = n * a.G;
     tiles = (int32_t)(((int64_t)rows + TM - 1) / TM);
-    lastw = FW + ((16 - FW) * (rows - (tiles - 1) * TM) + TM - 1) / TM;
+    const int32_t rest = rows - (tiles - 1) * TM;  // of the last tile
+    lastw = NR > 0 && rest <= 16 ? NR : FW + ((16 - FW) * rest + TM - 1) / TM;
   }
   // Units of tile t: the keys up to its last row (by whole tokens) and a constant, in 16ths.
   __device__ __forceinline__ int64_t step(const PagedArgs& a) const { return a.G < TM ? TM / a.G : 1; }
-  __device__ __forceinline__ int64_t fixed() const { return (base > 0 ? base : 0) + kOver<TM>; }
+  __device__ __forceinline__ int64_t past() const { return base > 0 ? base : 0; }
   __device__ __forceinline__ int64_t units(const PagedArgs& a, int64_t t) const {
-    return (fixed() + (t + 1) * step(a)) * (t == tiles - 1 ? lastw : 16);
+    return (past() + (t + 1) * step(a)) * (t == tiles - 1 ? lastw : 16) + 16 * kOver<TM>;
   }
   __device__ __forceinline__ int64_t before(const PagedArgs& a, int64_t t) const {  // of tiles 0 .. t - 1, t < tiles
-    return 16 * (t * fixed() + step(a) * (t * (t + 1) / 2));
+    return 16 * (t * (past() + kOver<TM>) + step(a) * (t * (t + 1) / 2));
   }
   __device__ __forceinline__ int64_t all(const PagedArgs& a) const {
     return tiles > 0 ? before(a, tiles - 1) + units(a, tiles - 1) : 0;
@@ -105,20 +106,20 @@ struct Cut {  // the line of units in n equal parts
 };
 
 // A workgroup's way along its part.
-template <int TM, int FW>
+template <int TM, int FW, int NR = 0>
 struct Walk {
   Cut cut;
   int32_t lw;     // the workgroup's place in the line
   int64_t x, x1;  // units done and to do
   int r, h, t;    // the tile at hand: request, KV head, tile of its rows
   int64_t u0, u1, units;  // this part of the tile's units, and all of them
-  Req<TM, FW> rq;
+  Req<TM, FW, NR> rq;
 
   // Finds the part's beginning; false: the workgroup has none. Every thread of the NT calls it.
   struct Found {
     int64_t x;
     int32_t r;
-    Req<TM, FW> rq;
+    Req<TM, FW, NR> rq;
   };
   template <int NT>
   __device__ __forceinline__ bool begin(const PagedArgs& a, int64_t* scan, Found* found) {
@@ -127,7 +128,7 @@ struct Walk {
     auto chunk = [&](int r0, int64_t& sum) __attribute__((always_inline)) {
       cost = 0;
       if (r0 + tid < a.R) {
-        rq = Req<TM, FW>(a, r0 + tid);
+        rq = Req<TM, FW, NR>(a, r0 + tid);
         cost = rq.all(a) * a.Hkv;
       }
       upto = block_scan<NT>(cost, sum, scan);
@@ -196,7 +197,7 @@ struct Walk {
         h = 0;
         do {
           if (++r >= a.R) return false;
-          rq = Req<TM, FW>(a, r);
+          rq = Req<TM, FW, NR>(a, r);
         } while (rq.tiles == 0);
       }
     }
