@@ -409,9 +409,11 @@ def lh_paged_workspace_bytes(pc) -> int:
 
 
 def _need_on(fn, t, name, dt, n, dev):
-    """A dense tensor of n elements or more of dtype dt on device dev."""
+    """The address of t: a dense tensor of n elements or more of dtype dt on device dev (an address or None passes)."""
     if t is None or isinstance(t, int):
-        return
+        return t
+    if t.dtype is dt and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
     if not t.is_cuda:
         raise LighthouseError(f"{fn}: {name} is not a device tensor")
     if t.get_device() != dev:
@@ -420,28 +422,26 @@ def _need_on(fn, t, name, dt, n, dev):
         raise LighthouseError(f"{fn}: {name} is not contiguous")
     if t.dtype != dt:
         raise LighthouseError(f"{fn}: {name} has dtype {t.dtype}, {dt} expected")
-    if t.numel() < n:
-        raise LighthouseError(f"{fn}: {name} has {t.numel()} elements, {n} needed")
+    raise LighthouseError(f"{fn}: {name} has {t.numel()} elements, {n} needed")
 
 
 def _need_rows(fn, t, name, dt, T, H, D, dev):
-    """[T, H, D] (or more rows) whose rows of H * D elements are dense; the stride between them, in elements."""
+    """[T, H, D] (or more rows) whose rows of H * D elements are dense: its address and the stride between them, in
+    elements."""
     if t is None or isinstance(t, int):
-        return H * D
-    if not t.is_cuda:
-        raise LighthouseError(f"{fn}: {name} is not a device tensor")
+        return t, H * D
+    shape, st = t.shape, t.stride()
     if t.get_device() != dev:
+        if not t.is_cuda:
+            raise LighthouseError(f"{fn}: {name} is not a device tensor")
         raise LighthouseError(f"{fn}: {name} is on device {t.get_device()}, the current one is {dev}")
     if t.dtype != dt:
         raise LighthouseError(f"{fn}: {name} has dtype {t.dtype}, {dt} expected")
-    shape, st = t.shape, t.stride()
     if len(shape) != 3 or shape[0] < T or shape[1] != H or shape[2] != D:
         raise LighthouseError(f"{fn}: {name} has shape {tuple(shape)}, ({T}, {H}, {D}) needed")
     if st[2] != 1 or (H > 1 and st[1] != D):
         raise LighthouseError(f"{fn}: {name} is not contiguous within a token")
-    if shape[0] == 1:
-        return H * D  # the stride of a single row says nothing
-    return st[0]
+    return t.data_ptr(), st[0] if shape[0] > 1 else H * D  # (the stride of a single row says nothing)
 
 
 def _xdt(pc):
@@ -449,42 +449,36 @@ def _xdt(pc):
 
 
 def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, balance, n_taken=None, stream=None):
-    fn, i32, dev = "lh_page_plan", torch.int32, _device()
-    for t, name, n in ((cached, "cached", pc.R), (fresh, "fresh", pc.R), (free_pages, "free_pages", pc.pages),
-                       (n_free, "n_free", 1), (table, "table", pc.R * pc.max_blocks), (cu_q, "cu_q", pc.R + 1),
-                       (kv_len, "kv_len", pc.R), (slots, "slots", pc.T), (pos, "pos", pc.T), (balance, "balance", 1),
-                       (n_taken, "n_taken", 1)):
-        _need_on(fn, t, name, i32, n, dev)
-    _call(fn, ctypes.byref(pc), _p(cached), _p(fresh), _p(free_pages), _p(n_free), _p(table), _p(cu_q), _p(kv_len),
-          _p(slots), _p(pos), _p(balance), _p(n_taken), _stream(stream))
+    fn, i32, dev, need = "lh_page_plan", torch.int32, _device(), _need_on
+    R, T = pc.R, pc.T
+    _call(fn, ctypes.byref(pc), need(fn, cached, "cached", i32, R, dev), need(fn, fresh, "fresh", i32, R, dev),
+          need(fn, free_pages, "free_pages", i32, pc.pages, dev), need(fn, n_free, "n_free", i32, 1, dev),
+          need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
+          need(fn, kv_len, "kv_len", i32, R, dev), need(fn, slots, "slots", i32, T, dev), need(fn, pos, "pos", i32, T, dev),
+          need(fn, balance, "balance", i32, 1, dev), need(fn, n_taken, "n_taken", i32, 1, dev), _stream(stream))
 
 
 def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
     """The strides of the C entry point are k's and v's own."""
-    fn, dt, dev = "lh_page_write", _xdt(pc), _device()
-    ks = _need_rows(fn, k, "k", dt, pc.T, pc.Hkv, pc.D, dev)
-    vs = _need_rows(fn, v, "v", dt, pc.T, pc.Hkv, pc.D, dev)
-    n = pc.pages * pc.Hkv * pc.page * pc.D
-    _need_on(fn, slots, "slots", torch.int32, pc.T, dev)
-    _need_on(fn, kpages, "kpages", dt, n, dev)
-    _need_on(fn, vpages, "vpages", dt, n, dev)
-    _call(fn, ctypes.byref(pc), _p(k), ks, _p(v), vs, _p(slots), _p(kpages), _p(vpages), _stream(stream))
+    fn, dt, dev, need = "lh_page_write", _xdt(pc), _device(), _need_on
+    T, H, D = pc.T, pc.Hkv, pc.D
+    n = pc.pages * H * pc.page * D
+    kp, ks = _need_rows(fn, k, "k", dt, T, H, D, dev)
+    vp, vs = _need_rows(fn, v, "v", dt, T, H, D, dev)
+    _call(fn, ctypes.byref(pc), kp, ks, vp, vs, need(fn, slots, "slots", torch.int32, T, dev),
+          need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev), _stream(stream))
 
 
 def lh_sdpa_paged(pc, q, kpages, vpages, table, cu_q, kv_len, o, lse, ws, ws_bytes=None, stream=None):
     """The stride of the C entry point is q's own; lse may be None."""
-    fn, dt, i32, dev = "lh_sdpa_paged", _xdt(pc), torch.int32, _device()
-    qs = _need_rows(fn, q, "q", dt, pc.T, pc.Hq, pc.D, dev)
-    n = pc.pages * pc.Hkv * pc.page * pc.D
-    _need_on(fn, kpages, "kpages", dt, n, dev)
-    _need_on(fn, vpages, "vpages", dt, n, dev)
-    _need_on(fn, table, "table", i32, pc.R * pc.max_blocks, dev)
-    _need_on(fn, cu_q, "cu_q", i32, pc.R + 1, dev)
-    _need_on(fn, kv_len, "kv_len", i32, pc.R, dev)
-    _need_on(fn, o, "o", dt, pc.T * pc.Hq * pc.D, dev)
-    _need_on(fn, lse, "lse", torch.float32, pc.T * pc.Hq, dev)
-    _need_on(fn, ws, "ws", torch.uint8, ws_bytes or 0, dev)
-    _call(fn, ctypes.byref(pc), _p(q), qs, _p(kpages), _p(vpages), _p(table), _p(cu_q), _p(kv_len), _p(o), _p(lse), _p(ws),
+    fn, dt, i32, dev, need = "lh_sdpa_paged", _xdt(pc), torch.int32, _device(), _need_on
+    R, T, H, D = pc.R, pc.T, pc.Hq, pc.D
+    n = pc.pages * pc.Hkv * pc.page * D
+    qp, qs = _need_rows(fn, q, "q", dt, T, H, D, dev)
+    _call(fn, ctypes.byref(pc), qp, qs, need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev),
+          need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
+          need(fn, kv_len, "kv_len", i32, R, dev), need(fn, o, "o", dt, T * H * D, dev),
+          need(fn, lse, "lse", torch.float32, T * H, dev), need(fn, ws, "ws", torch.uint8, ws_bytes or 0, dev),
           _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream))
 
 

