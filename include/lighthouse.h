@@ -311,8 +311,8 @@ typedef struct {
   int32_t max_blocks;  /* columns of the table, >= 1: a request holds max_blocks * page tokens      */
   int64_t T;           /* rows of q, k, v, o, >= 1 (rows behind the last request's are not touched) */
   int64_t pages;       /* pages of the cache, >= 1; pages * page < 2^31                             */
-  int32_t page;        /* tokens of a page: a power of two, 16 .. 1024; max_blocks * page < 2^31   */
-  int32_t Hq, Hkv;     /* heads, Hq % Hkv == 0 (query head hq reads KV head hq / (Hq / Hkv)); T * Hq < 2^31 */
+  int32_t page;        /* tokens of a page: a power of two, 16 .. 1024; max_blocks * page <= 2^30  */
+  int32_t Hq, Hkv;     /* heads, Hq % Hkv == 0 (query head hq reads KV head hq / (Hq / Hkv)); T * Hq <= 2^30 */
   int32_t D;           /* head dimension: 64 or 128                                                */
   int32_t dtype;       /* lh_dtype of q, k, v, o and the pages                                     */
   float scale;         /* softmax scale, finite and >= 0; 0 selects 1/sqrt(D)                      */

@@ -8,7 +8,7 @@
 
 namespace {
 
-constexpr int64_t k2G = (int64_t)1 << 31;
+constexpr int64_t k2G = (int64_t)1 << 31, k1G = (int64_t)1 << 30;
 
 lh_status make_paged(const lh_paged* pc, LhPaged* s) {
   if (!pc) return lh_fail(LH_E_NULL, "the step's description is NULL");
@@ -28,9 +28,10 @@ lh_status make_paged(const lh_paged* pc, LhPaged* s) {
   if (pc->scale < 0.0f) return lh_fail(LH_E_PARAM, "scale must be >= 0 (0 selects 1/sqrt(D))");
   if (pc->pages >= k2G / pc->page)
     return lh_fail(LH_E_SHAPE, "the cache has %lld * %d >= 2^31 slots", (long long)pc->pages, pc->page);
-  if (pc->max_blocks >= k2G / pc->page)
-    return lh_fail(LH_E_SHAPE, "a request could hold %d * %d >= 2^31 tokens", pc->max_blocks, pc->page);
-  if (pc->T >= k2G / pc->Hq) return lh_fail(LH_E_SHAPE, "T * Hq = %lld * %d >= 2^31", (long long)pc->T, pc->Hq);
+  // (the kernels count a request's keys and rows in 32 bits, and look up to a tile further)
+  if (pc->max_blocks > k1G / pc->page)
+    return lh_fail(LH_E_SHAPE, "a request could hold %d * %d > 2^30 tokens", pc->max_blocks, pc->page);
+  if (pc->T > k1G / pc->Hq) return lh_fail(LH_E_SHAPE, "T * Hq = %lld * %d > 2^30", (long long)pc->T, pc->Hq);
   memset(s, 0, sizeof(*s));
   s->T = pc->T, s->pages = pc->pages, s->R = pc->R, s->max_blocks = pc->max_blocks, s->page = pc->page;
   while ((1 << s->shift) < s->page) ++s->shift;

@@ -99,10 +99,21 @@ struct Req {
   }
 };
 
-struct Cut {  // the line of units in n equal parts
+// floor(a / b), a >= 0, b > 0. (The 64-bit integer division is longer, and several stand before the first load of a part.)
+// The first quotient is off by 2^-52 of itself and one at most, so the rest is a few b's, whose quotient is exact but for
+// one.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  int64_t q = (int64_t)((double)a / (double)b);
+  int64_t r = a - q * b;
+  const int64_t more = (int64_t)((double)r / (double)b);
+  q += more, r -= more * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
+
+struct Cut {  // the line of units in n equal parts, the first `rem` of them one longer
   int64_t q, rem;
   int32_t n;
-  __device__ __forceinline__ int64_t start(int64_t w) const { return q * w + rem * w / n; }
+  __device__ __forceinline__ int64_t start(int64_t w) const { return q * w + (w < rem ? w : rem); }
 };
 
 // A workgroup's way along its part.
@@ -138,10 +149,10 @@ struct Walk {
       __syncthreads();
     };
     for (int r0 = 0; r0 < a.R; r0 += NT) chunk(r0, total);
-    const int64_t most = (total + 16 * kLeast<TM> - 1) / (16 * kLeast<TM>);
+    const int64_t most = (total + 16 * kLeast<TM> - 1) / (16 * kLeast<TM>);  // (a power of two)
     // (between one and two workgroups a CU, those that share one would take twice as long)
     cut.n = most >= a.W ? a.W : most > kCUs ? kCUs : most <= 8 ? 8 : (int32_t)((most + 7) & ~7);
-    cut.q = total / cut.n, cut.rem = total - cut.q * cut.n;
+    cut.q = uni64(quotient(total, cut.n)), cut.rem = total - cut.q * cut.n;
     // neighbouring parts on one XCD (workgroups go to the 8 XCDs in turn): they read the same keys
     const int b = blockIdx.x;
     lw = b < cut.n ? (b % 8) * (cut.n / 8) + b / 8 : b;
@@ -169,7 +180,7 @@ struct Walk {
     rq.first = uni(rq.first), rq.n = uni(rq.n), rq.base = uni(rq.base);
     rq.rows = uni(rq.rows), rq.tiles = uni(rq.tiles), rq.lastw = uni(rq.lastw);
     const int64_t each = rq.all(a);
-    h = (int)(u0 / each);
+    h = uni((int)quotient(u0, each));
     u0 -= h * each;
     t = 0;
     int hi = rq.tiles;  // before(t) <= u0, and u0 < before(hi) or hi is behind the last
@@ -204,10 +215,11 @@ struct Walk {
     span(a);
     return true;
   }
-  // This part's share [b0, b1) of the tile's nb blocks of keys: parts that meet agree on the block between them.
+  // This part's share [b0, b1) of the tile's nb blocks of keys. Parts that meet agree on the block between them: it is
+  // the same expression of the same unit, does not fall where the unit grows, and is nb at most.
   __device__ __forceinline__ void blocks(int nb, int& b0, int& b1) const {
-    b0 = (int)(nb * u0 / units);
-    b1 = u1 == units ? nb : (int)(nb * u1 / units);
+    b0 = u0 == 0 ? 0 : (int)((double)nb * (double)u0 / (double)units);
+    b1 = u1 == units ? nb : (int)((double)nb * (double)u1 / (double)units);
   }
   __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == units; }
   __device__ __forceinline__ int64_t slot() const { return 2 * (int64_t)lw + (u0 > 0 ? 0 : 1); }

@@ -233,6 +233,44 @@ def test_rows_without_a_key(shape, dtype):
     assert bool((o[a:x["cu"][2]] == 0).all()) and bool((lse[a:x["cu"][2]] == -float("inf")).all())
 
 
+@pytest.mark.parametrize("R,new,Hq,Hkv,dtype", [(700, (0, 1), 4, 2, BF), (4096, (1, 1), 2, 2, F32), (600, (4, 20), 16, 1, BF),
+                                                (900, (20, 40), 8, 1, BF), (300, (1, 5), 8, 2, F32)])
+def test_more_requests_than_threads(R, new, Hq, Hkv, dtype):
+    """The cut of the work sums over the requests a workgroup's threads at a time."""
+    print(f"[attend many] R={R} new={new} {Hq}/{Hkv} {dtype}", flush=True)
+    rng = random.Random(R)
+    lens = [(rng.choice([0, 3, 16, rng.randrange(60)]), rng.randint(*new)) for _ in range(R)]
+    x = _setup(lens, Hq, Hkv, 64, 16, dtype, seed=R)
+    _check(x, *_run(x))
+
+
+@pytest.mark.parametrize("D,dtype", [(128, BF), (64, BF), (128, F32)])
+def test_random_steps(D, dtype):
+    """Lengths, heads and pages at random: every variant of the kernels and tiles that parts divide anywhere."""
+    rng = random.Random(D + (dtype == F32))
+    for i in range(14):
+        Hkv = rng.choice([1, 2, 3])
+        Hq = Hkv * rng.choice([1, 2, 3, 4, 6, 8])
+        most = rng.choice([1, 2, 8, 40, 200, 500])
+        lens = [(rng.choice([0, 1, 15, 64, rng.randrange(3000)]), rng.choice([0, 1, 1, most, rng.randint(1, most)]))
+                for _ in range(rng.choice([1, 2, 5, 12, 30]))]
+        page = rng.choice([16, 32, 64, 128])
+        print(f"[attend random] {i} D={D} {dtype} {Hq}/{Hkv} page={page} lens={lens}", flush=True)
+        x = _setup(lens, Hq, Hkv, D, page, dtype, seed=i, fused=rng.random() < 0.5)
+        _check(x, *_run(x))
+
+
+def test_without_lse():
+    print("[attend] no lse", flush=True)
+    for name in ("decode", "mixed"):
+        x = _setup(STEPS[name], 8, 2, 64, 16, BF, seed=61)
+        o, _ = _run(x)
+        o2 = torch.full_like(o, 7.0)
+        lh.lh_sdpa_paged(x["pc"], x["q"], x["kp"], x["vp"], _i(x["table"]), _i(x["cu"]), _i(x["kv"]), o2, None,
+                         lh.paged_workspace(x["pc"]))
+        assert torch.equal(o, o2)
+
+
 def test_step_without_rows():
     print("[attend] no rows", flush=True)
     x = _setup([(20, 0), (0, 0)], 4, 2, 64, 16, BF, T=5)
@@ -486,3 +524,33 @@ def test_two_steps_at_once():
     torch.cuda.synchronize()
     for (o, lse, *_), (ro, rl), x in zip(bufs, refs, xs):
         assert torch.equal(o[:x["rows"]], ro[:x["rows"]]) and torch.equal(lse[:x["rows"]], rl[:x["rows"]])
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured steps with one workspace, replayed in turn: nothing of one call is left for another."""
+    print("[two graphs]", flush=True)
+    xs = [_setup(STEPS["decode"], 8, 2, 128, 16, BF, seed=71), _setup(STEPS["mixed"], 8, 2, 128, 16, BF, seed=72)]
+    refs = [_run(x) for x in xs]
+    need = max(lh.lh_paged_workspace_bytes(x["pc"]) for x in xs)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    graphs, outs = [], []
+    for x in xs:
+        pc = x["pc"]
+        args = (_i(x["table"]), _i(x["cu"]), _i(x["kv"]), torch.empty(x["T"], pc.Hq, pc.D, dtype=BF, device=DEV),
+                torch.empty(x["T"], pc.Hq, device=DEV), ws)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            lh.lh_sdpa_paged(pc, x["q"], x["kp"], x["vp"], *args)
+        torch.cuda.current_stream().wait_stream(s)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            lh.lh_sdpa_paged(pc, x["q"], x["kp"], x["vp"], *args)
+        graphs.append(g), outs.append(args)
+    for rep in range(4):
+        for g, args, (ro, rl), x in zip(graphs, outs, refs, xs):
+            args[3].zero_(), args[4].zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            n = x["rows"]
+            assert torch.equal(args[3][:n], ro[:n]) and torch.equal(args[4][:n], rl[:n]), f"replay {rep}"

@@ -23,8 +23,8 @@ def _pc(**kw):
     (dict(dtype=2), -4), (dict(dtype=torch.float32), 0),
     (dict(scale=float("nan")), -8), (dict(scale=float("inf")), -8), (dict(scale=-1.0), -3), (dict(scale=0.5), 0),
     (dict(pages=2 ** 27 - 1), 0), (dict(pages=2 ** 27), -2),          # pages * page < 2^31
-    (dict(max_blocks=2 ** 27 - 1), 0), (dict(max_blocks=2 ** 27), -2),
-    (dict(T=2 ** 28 - 1), 0), (dict(T=2 ** 28), -2),                 # T * Hq < 2^31
+    (dict(max_blocks=2 ** 26), 0), (dict(max_blocks=2 ** 26 + 1), -2),  # max_blocks * page <= 2^30
+    (dict(T=2 ** 27), 0), (dict(T=2 ** 27 + 1), -2),                  # T * Hq <= 2^30
 ])
 def test_check_codes(kw, code):
     pc = _pc(**kw)
