@@ -21,7 +21,7 @@ struct PlanArgs {
 // every workgroup forms the sums for itself (R lengths, which the caches hold) and then maps
 // its own range of tokens, and nothing waits for another workgroup. The table entry of a new page is
 // written by its first token, which is always one of the step's.
-// Bound by the latency of the launch and of the two scans.
+// Bound by the latency of the launch and of the two scans: 64 requests of one token 4.0 us, 256 of 203,000 tokens 5.7.
 constexpr int kPlanThreads = 256;  // a token a thread: with four, 203,000 tokens of 256 requests take 7.7 us and not 5.7
 
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs a) {
@@ -111,7 +111,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PlanArgs 
 
 // A thread moves one 16-byte chunk of a K row and the same chunk of the V row. Rows of a head are
 // 128 to 512 consecutive bytes on both sides, so a wave reads and writes whole lines. Bound by
-// HBM: each row is read and written once.
+// HBM: each row is read and written once (24,548 tokens of 8 heads of 128 in bf16, 201 MB: 33 us, 6.0 TB/s; one
+// token of each of 64 requests 2.6 us, the launch).
 __global__ void __launch_bounds__(256)
 page_write_kernel(const char* __restrict__ k, int64_t k_stride, const char* __restrict__ v, int64_t v_stride,
                   const int32_t* __restrict__ slots, char* __restrict__ kp, char* __restrict__ vp, uint32_t rows,
