@@ -149,13 +149,22 @@ __device__ __forceinline__ void rows_tile(const PagedArgs& a, const RowsItem& it
     if constexpr (B16) {
       // The weights as the sum of two bf16 values, whose products are both formed: the matrix unit has time for it
       // beside the loads, and o is off by its own rounding alone (2-norm 1.65e-3; with the weights rounded once 2.3e-3).
+      // The first is cut off, not rounded, and the last bit set: the second is above 0 wherever the weight is, so that
+      // an infinite value of V keeps its sign in both products. (In all within 2^-16 of the weight.)
       bf16x8 pb[RT], pl[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        pb[rt] = cvt8(p[rt]);
+        u32v4 hi;
         float rest[C::NV];
 #pragma unroll
-        for (int i = 0; i < C::NV; ++i) rest[i] = p[rt][i] - (float)pb[rt][i];
+        for (int i = 0; i < C::NV; ++i) {
+          const uint32_t x = __float_as_uint(p[rt][i]);
+          rest[i] = __uint_as_float(x | 1u) - __uint_as_float(x & 0xffff0000u);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          hi[c] = __builtin_amdgcn_perm(__float_as_uint(p[rt][2 * c + 1]), __float_as_uint(p[rt][2 * c]), 0x07060302u);
+        pb[rt] = __builtin_bit_cast(bf16x8, hi);
         pl[rt] = cvt8(rest);
       }
 #pragma unroll

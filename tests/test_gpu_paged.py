@@ -308,6 +308,30 @@ def test_a_rows_odd_values_reach_no_earlier_row(lens, bad, dtype):
             assert bool(torch.isnan(o[after][:, :2]).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens", [[(300, 1)], [(300, 1), (40, 0), (5000, 3)], [(300, 9), (20, 7)], [(300, 40), (100, 1)],
+                                  [(300, 200), (700, 1), (64, 100)]])
+def test_infinite_values_that_rows_see(lens, dtype):
+    """Infinities and NaN of V among the first keys, which all rows see: their columns hold what the sum over the keys
+    does (one sign: that infinity; both, or NaN: NaN), the others are as they were."""
+    print(f"[attend seen odd] {lens} {dtype}", flush=True)
+    for D, Hq in ((64, 4), (128, 8)):
+        x = _setup(lens, Hq, 2, D, 16, dtype, seed=31)
+        x["q"] = x["q"] * 0.25  # logits of a few units: no weight vanishes
+        clean, _ = _run(x)
+        inf = float("inf")
+        for r in range(len(lens)):
+            page = x["vp"][x["table"][r][0]]
+            for key, col, bad in ((3, 0, inf), (5, 1, -inf), (9, 2, float("nan")), (2, 3, inf), (15, 3, -inf), (4, D - 1, inf), (12, D - 1, inf)):
+                page[1, key, col] = bad
+        o, lse = _run(x)
+        _check(x, o, lse)
+        half = Hq // 2
+        assert torch.equal(o[:, :half], clean[:, :half]) and torch.equal(o[:, :, 4:D - 1], clean[:, :, 4:D - 1])
+        assert bool((o[:x["rows"], half:, 0] == inf).all()) and bool((o[:x["rows"], half:, 1] == -inf).all())
+        assert bool(torch.isnan(o[:x["rows"], half:, 2:4]).all()) and bool((o[:x["rows"], half:, D - 1] == inf).all())
+
+
 def test_large_logits():
     """Logits in the thousands, where a weight is 0 or 1, and runs of growing maxima."""
     print("[attend large logits]", flush=True)
