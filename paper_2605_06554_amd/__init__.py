@@ -8,6 +8,7 @@ call fails, the error is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -578,6 +579,13 @@ def attention_backward(pr, state, dout, stream=None):
     return dq, dk, dv
 
 
+def _on(stream):
+    """Allocations inside belong to `stream`: memory that is freed is not handed out before its work is done."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
 def paged_workspace(pc, device="cuda"):
     """A device byte buffer of lh_paged_workspace_bytes(pc) bytes. Calls that may run at the same time (two
     streams, two captured graphs) need one each."""
@@ -593,17 +601,20 @@ def page_plan(pc, cached, fresh, free_pages, n_free, table, stream=None):
     """Allocates the outputs and runs lh_page_plan. Returns a dict of cu_q, kv_len, slots, pos, balance and n_taken;
     the new entries of table are written in place. The next step's n_free is this one's less n_taken."""
     e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)  # noqa: E731
-    out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), balance=e(1), n_taken=e(1))
+    with _on(stream):
+        out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), balance=e(1), n_taken=e(1))
     lh_page_plan(pc, cached, fresh, free_pages, n_free, table, *out.values(), stream=stream)
     return out
 
 
 def attention_paged(pc, q, k, v, kpages, vpages, table, plan, ws=None, stream=None):
     """One layer's attention of a step: writes k and v into the cache and attends with q, by the plan of
-    page_plan (the same for every layer of the step). Returns (o, lse)."""
+    page_plan (the same for every layer of the step). Returns (o, lse), whose rows behind the last request's are not
+    written."""
     lh_page_write(pc, k, v, plan["slots"], kpages, vpages, stream=stream)
-    o = torch.empty(pc.T, pc.Hq, pc.D, dtype=q.dtype, device=q.device)
-    lse = torch.empty(pc.T, pc.Hq, dtype=torch.float32, device=q.device)
-    ws = paged_workspace(pc, q.device) if ws is None else ws
+    with _on(stream):
+        o = torch.empty(pc.T, pc.Hq, pc.D, dtype=q.dtype, device=q.device)
+        lse = torch.empty(pc.T, pc.Hq, dtype=torch.float32, device=q.device)
+        ws = paged_workspace(pc, q.device) if ws is None else ws
     lh_sdpa_paged(pc, q, kpages, vpages, table, plan["cu_q"], plan["kv_len"], o, lse, ws, stream=stream)
     return o, lse

@@ -32,6 +32,11 @@ lh_status make_paged(const lh_paged* pc, LhPaged* s) {
   if (pc->max_blocks > k1G / pc->page)
     return lh_fail(LH_E_SHAPE, "a request could hold %d * %d > 2^30 tokens", pc->max_blocks, pc->page);
   if (pc->T > k1G / pc->Hq) return lh_fail(LH_E_SHAPE, "T * Hq = %lld * %d > 2^30", (long long)pc->T, pc->Hq);
+  // (units of the cut of an attention's work, whatever cu_q and kv_len hold: rows of 16 heads and up, keys in 16ths)
+  const unsigned __int128 units = (unsigned __int128)pc->R * (uint64_t)(pc->T * pc->Hq + 16 * (int64_t)pc->Hkv) *
+                                  (uint64_t)((int64_t)pc->max_blocks * pc->page + pc->T + 1024);
+  if (units > ((unsigned __int128)1 << 62))
+    return lh_fail(LH_E_SHAPE, "R * (T * Hq + 16 * Hkv) * (max_blocks * page + T + 1024) is above 2^62");
   memset(s, 0, sizeof(*s));
   s->T = pc->T, s->pages = pc->pages, s->R = pc->R, s->max_blocks = pc->max_blocks, s->page = pc->page;
   while ((1 << s->shift) < s->page) ++s->shift;
@@ -53,6 +58,34 @@ lh_status need_stride(const LhPaged& s, int64_t stride, int32_t H, const char* n
   if (stride % (s.dtype == LH_BF16 ? 8 : 4) != 0)
     return lh_fail(LH_E_ALIGN, "%s = %lld elements is not a multiple of 16 bytes", name, (long long)stride);
   if (stride > ((int64_t)1 << 40)) return lh_fail(LH_E_SHAPE, "%s = %lld is out of range", name, (long long)stride);
+  return LH_OK;
+}
+
+// An array of a call, in bytes. (No size is within 64 bits for all bounds that pass the checks.)
+typedef unsigned __int128 u128;
+struct Span {
+  const char* name;
+  const void* at;
+  u128 bytes;
+};
+u128 rows_bytes(const LhPaged& s, int64_t stride, int32_t H) {
+  return ((u128)(s.T - 1) * (uint64_t)stride + (uint64_t)H * s.D) * (s.dtype == LH_BF16 ? 2 : 4);
+}
+u128 pool_bytes(const LhPaged& s) {
+  return (u128)(uint64_t)(s.pages * s.page) * (uint64_t)((int64_t)s.Hkv * s.D * (s.dtype == LH_BF16 ? 2 : 4));
+}
+// The last `n_out` of the arrays are written: none of them may share memory with another array. (Workgroups read
+// the inputs while others write.)
+template <int N>
+lh_status need_apart(const Span (&x)[N], int n_out) {
+  for (int i = N - n_out; i < N; ++i) {
+    if (!x[i].at) continue;
+    for (int j = 0; j < i; ++j) {
+      const uintptr_t a = (uintptr_t)x[i].at, b = (uintptr_t)x[j].at;
+      if (b && (u128)a < b + x[j].bytes && (u128)b < a + x[i].bytes)
+        return lh_fail(LH_E_PARAM, "%s and %s overlap", x[j].name, x[i].name);
+    }
+  }
   return LH_OK;
 }
 
@@ -100,6 +133,11 @@ lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t*
   LH_TRY(need(pos, "pos", 4));
   LH_TRY(need(balance, "balance", 4));
   if (n_taken) LH_TRY(need(n_taken, "n_taken", 4));
+  const u128 R = 4 * (u128)s.R, T = 4 * (u128)s.T;
+  LH_TRY(need_apart({{"cached", cached, R}, {"fresh", fresh, R}, {"free_pages", free_pages, 4 * (u128)s.pages},
+                     {"n_free", n_free, 4}, {"table", table, R * s.max_blocks}, {"cu_q", cu_q, R + 4},
+                     {"kv_len", kv_len, R}, {"slots", slots, T}, {"pos", pos, T}, {"balance", balance, 4},
+                     {"n_taken", n_taken, 4}}, 7));
   lh_fail(LH_OK, "%s", "");
   return status(lh_launch_page_plan(s, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slots, pos, balance,
                                     n_taken, (hipStream_t)stream),
@@ -117,6 +155,8 @@ lh_status lh_page_write(const lh_paged* pc, const void* k, int64_t k_stride, con
   LH_TRY(need(slots, "slots", 4));
   LH_TRY(need(kpages, "kpages", 16));
   LH_TRY(need(vpages, "vpages", 16));
+  LH_TRY(need_apart({{"k", k, rows_bytes(s, k_stride, s.Hkv)}, {"v", v, rows_bytes(s, v_stride, s.Hkv)},
+                     {"slots", slots, 4 * (u128)s.T}, {"kpages", kpages, pool_bytes(s)}, {"vpages", vpages, pool_bytes(s)}}, 2));
   lh_fail(LH_OK, "%s", "");
   return status(lh_launch_page_write(s, k, k_stride, v, v_stride, slots, kpages, vpages, (hipStream_t)stream),
                 "lh_page_write");
@@ -142,6 +182,11 @@ lh_status lh_sdpa_paged(const lh_paged* pc, const void* q, int64_t q_stride, con
     if (((uintptr_t)ws & 255u) != 0) return lh_fail(LH_E_ALIGN, "workspace is not 256-byte aligned");
     if (ws_bytes < bytes) return lh_fail(LH_E_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, bytes);
   }
+  LH_TRY(need_apart({{"q", q, rows_bytes(s, q_stride, s.Hq)}, {"kpages", kpages, pool_bytes(s)},
+                     {"vpages", vpages, pool_bytes(s)}, {"table", table, 4 * (u128)s.R * s.max_blocks},
+                     {"cu_q", cu_q, 4 * (u128)s.R + 4}, {"kv_len", kv_len, 4 * (u128)s.R},
+                     {"o", o, rows_bytes(s, (int64_t)s.Hq * s.D, s.Hq)}, {"lse", lse, 4 * (u128)s.T * s.Hq},
+                     {"ws", ws, bytes}}, 3));
   lh_fail(LH_OK, "%s", "");
   return status(lh_launch_sdpa_paged(s, q, q_stride, kpages, vpages, table, cu_q, kv_len, o, lse, ws,
                                      (hipStream_t)stream),

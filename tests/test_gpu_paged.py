@@ -382,6 +382,34 @@ def test_same_call_same_bits_on_another_stream():
             assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+def test_helpers_on_another_stream():
+    """page_plan and attention_paged with a stream of their own (as an object, its address, and the null stream's) and
+    a workspace that they allocate: the results are the default stream's, also where memory freed there is taken again at once."""
+    print("[attend] helpers on another stream", flush=True)
+    R, page, Hq, Hkv, D = 5, 16, 8, 2, 64
+    cached, fresh = [0] * R, [40, 1, 300, 17, 64]
+    T, pages, width = sum(fresh), 40, 20
+    pc = lh.paged(R, width, T, pages, page, Hq, Hkv, D)
+    g = torch.Generator(DEV).manual_seed(5)
+    q, k, v = (torch.randn(T, h, D, generator=g, device=DEV).to(BF) for h in (Hq, Hkv, Hkv))
+    args = _i(cached), _i(fresh), _i(list(range(pages))), _i([pages])
+    side = torch.cuda.Stream()
+    outs = []
+    for stream in (None, side, side.cuda_stream, 0):
+        table = torch.full((R, width), -1, dtype=I32, device=DEV)
+        kp, vp = lh.paged_cache(pages, page, Hkv, D)
+        torch.cuda.synchronize()
+        plan = lh.page_plan(pc, *args, table, stream=stream)
+        for _ in range(3):
+            o, lse = lh.attention_paged(pc, q, k, v, kp, vp, table, plan, stream=stream)
+            torch.full((1 << 24,), 255, dtype=torch.uint8, device=DEV)  # (takes what the default stream has free)
+        torch.cuda.synchronize()
+        outs.append((o.clone(), lse.clone(), table.clone()))
+    assert bool(torch.isfinite(outs[0][0].float()).all())
+    for got in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got, outs[0]))
+
+
 def test_pool_beyond_32_bit_offsets():
     """A pool of more than 2^32 bytes (and elements past 2^31): a request on its last pages."""
     print("[attend large pool]", flush=True)

@@ -25,6 +25,9 @@ def _pc(**kw):
     (dict(pages=2 ** 27 - 1), 0), (dict(pages=2 ** 27), -2),          # pages * page < 2^31
     (dict(max_blocks=2 ** 26), 0), (dict(max_blocks=2 ** 26 + 1), -2),  # max_blocks * page <= 2^30
     (dict(T=2 ** 27), 0), (dict(T=2 ** 27 + 1), -2),                  # T * Hq <= 2^30
+    (dict(R=16, T=2 ** 27 - 4, max_blocks=2 ** 24), -2),              # 2^34 (2^28 + 2^27) > 2^62 units of the cut
+    (dict(R=8, T=2 ** 27 - 4, max_blocks=2 ** 24), 0),
+    (dict(R=4096, T=2 ** 27, max_blocks=2 ** 26), -2), (dict(R=4096, T=8192, Hq=32, Hkv=8, max_blocks=2 ** 26), 0),
 ])
 def test_check_codes(kw, code):
     pc = _pc(**kw)
@@ -75,6 +78,39 @@ def test_null_and_misaligned_pointers():
             bad[i] = value
             assert lib.lh_sdpa_paged(by, *bad, None) == code
     assert lib.lh_sdpa_paged(ctypes.byref(_pc(D=32)), *good, None) == -3
+
+
+def test_overlapping_arrays():
+    """An output that shares memory with another array of its call is refused; inputs may share theirs."""
+    lib, pc = lh._load(), _pc()
+    by = ctypes.byref(pc)
+    size = [16, 16, 256, 4, 128, 20, 16, 400, 400, 4, 4]  # bytes of the plan's arrays; the last seven are outputs
+    at, good = 1 << 20, []
+    for n in size:
+        good.append(at)
+        at += n
+    for i in range(4, 11):
+        for j in range(i):
+            for where in (good[j] + size[j] - 4, good[j] - size[i] + 4):  # the last word of it, and the first
+                bad = list(good)
+                bad[i] = where
+                assert lib.lh_page_plan(by, *bad, None) == -3 and "overlap" in lh.lh_last_error(), (i, j)
+    row, rows, pool = 2 * 64, 100 * 2 * 64 * 2, 64 * 2 * 16 * 64 * 2
+    M = 1 << 24
+    k, v, slots, kp, vp = M, 2 * M, 3 * M, 4 * M, 5 * M
+    for a in ((k, v, slots, kp, kp), (k, v, slots, kp, kp + pool - 16), (k, v, slots, k + rows - 16, vp), (k, v, slots, k - pool + 16, vp),
+              (k, v, slots, v, vp), (k, v, slots, kp, k), (k, v, vp + 64, kp, vp), (kp, v, slots, kp, vp)):
+        assert lib.lh_page_write(by, a[0], row, a[1], row, *a[2:], None) == -3, a
+        assert "overlap" in lh.lh_last_error()
+    assert lib.lh_page_write(by, k, 2 * row, v, row, slots, k + 2 * rows - 2 * row - 16, vp, None) == -3  # the last row's end
+    need = lh.lh_paged_workspace_bytes(pc)
+    q, table, cu, kv, o, lse, ws = M, 6 * M, 7 * M, 8 * M, 9 * M, 10 * M, 1 << 32
+    good = [q, 8 * 64, kp, vp, table, cu, kv, o, lse, ws, need]
+    for i, where in ((7, q), (7, kp + pool - 16), (7, vp), (7, table), (8, o + 100 * 8 * 64 * 2 - 4), (8, cu + 16), (9, o), (9, lse & -256),
+                     (4, ws + 64), (6, lse), (0, ws + need - 256), (8, kv)):
+        bad = list(good)
+        bad[i] = where
+        assert lib.lh_sdpa_paged(by, *bad, None) == -3 and "overlap" in lh.lh_last_error(), (i, hex(where))
 
 
 class _Fake:
