@@ -156,10 +156,11 @@ def _p(t):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream):
+def _stream(stream, dev=None):
+    """The stream's address; without one, that of the current stream of dev, the current device (looked up if not given)."""
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch.cuda.current_device() if dev is None else dev)
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -411,10 +412,13 @@ def lh_paged_workspace_bytes(pc) -> int:
 
 def _need_on(fn, t, name, dt, n, dev):
     """The address of t: a dense tensor of n elements or more of dtype dt on device dev (an address or None passes)."""
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype is dt and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
-        return t.data_ptr()
+    try:
+        if t.dtype is dt and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        if t is None or isinstance(t, int):
+            return t
+        raise
     if not t.is_cuda:
         raise LighthouseError(f"{fn}: {name} is not a device tensor")
     if t.get_device() != dev:
@@ -456,7 +460,7 @@ def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slo
           need(fn, free_pages, "free_pages", i32, pc.pages, dev), need(fn, n_free, "n_free", i32, 1, dev),
           need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
           need(fn, kv_len, "kv_len", i32, R, dev), need(fn, slots, "slots", i32, T, dev), need(fn, pos, "pos", i32, T, dev),
-          need(fn, balance, "balance", i32, 1, dev), need(fn, n_taken, "n_taken", i32, 1, dev), _stream(stream))
+          need(fn, balance, "balance", i32, 1, dev), need(fn, n_taken, "n_taken", i32, 1, dev), _stream(stream, dev))
 
 
 def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
@@ -467,7 +471,7 @@ def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
     kp, ks = _need_rows(fn, k, "k", dt, T, H, D, dev)
     vp, vs = _need_rows(fn, v, "v", dt, T, H, D, dev)
     _call(fn, ctypes.byref(pc), kp, ks, vp, vs, need(fn, slots, "slots", torch.int32, T, dev),
-          need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev), _stream(stream))
+          need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev), _stream(stream, dev))
 
 
 def lh_sdpa_paged(pc, q, kpages, vpages, table, cu_q, kv_len, o, lse, ws, ws_bytes=None, stream=None):
@@ -480,7 +484,7 @@ def lh_sdpa_paged(pc, q, kpages, vpages, table, cu_q, kv_len, o, lse, ws, ws_byt
           need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
           need(fn, kv_len, "kv_len", i32, R, dev), need(fn, o, "o", dt, T * H * D, dev),
           need(fn, lse, "lse", torch.float32, T * H, dev), need(fn, ws, "ws", torch.uint8, ws_bytes or 0, dev),
-          _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream))
+          _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream, dev))
 
 
 # ---------------------------------------------------------------- allocation helpers
