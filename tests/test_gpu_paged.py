@@ -446,6 +446,42 @@ def _serve(pc, state, q, k, v, cached, fresh, ws):
     return plan, o, lse
 
 
+@pytest.mark.parametrize("dtype,T,Hq,Hkv,new", [(BF, 300000, 64, 2, 75), (F32, 280000, 64, 64, 70)])
+def test_rows_beyond_32_bit_offsets(dtype, T, Hq, Hkv, new):
+    """More than 2^31 elements of q and o: the first and the last requests' rows against the definition."""
+    print(f"[attend] rows beyond 32-bit offsets {dtype}", flush=True)
+    D, page, R = 128, 128, T // new
+    assert T * Hq * D > 2 ** 31 and R * new == T
+    g = torch.Generator(DEV).manual_seed(3)
+    pc = lh.paged(R, 1, T, R, page, Hq, Hkv, D, dtype)
+    q = torch.empty(T, Hq, D, dtype=dtype, device=DEV).normal_(generator=g)
+    kp, vp = (torch.empty(R, Hkv, page, D, dtype=dtype, device=DEV).normal_(generator=g) for _ in range(2))
+    table = torch.arange(R - 1, -1, -1, dtype=I32, device=DEV)[:, None].contiguous()
+    cu, kv = torch.arange(0, T + 1, new, dtype=I32, device=DEV), torch.full((R,), new + 10, dtype=I32, device=DEV)
+    o, lse = torch.full((T, Hq, D), 7.0, dtype=dtype, device=DEV), torch.full((T, Hq), 7.0, device=DEV)
+    lh.lh_sdpa_paged(pc, q, kp, vp, table, cu, kv, o, lse, lh.paged_workspace(pc))
+    torch.cuda.synchronize()
+    for r in (0, R // 2, R - 1):
+        a, b = r * new, r * new + new
+        ref = paged_ref.attend(q[a:b], kp, vp, [[R - 1 - r]], [0, new], [new + 10], page)
+        paged_ref.check("o", o[a:b], ref[0], ref[2])
+        paged_ref.check("lse", lse[a:b], ref[1], ref[3])
+    assert bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_requests_that_share_pages(dtype):
+    """Requests whose tables name the same pages (a common beginning), and one page twice in a table: each reads them as
+    its own."""
+    print(f"[attend] shared pages {dtype}", flush=True)
+    for lens in ([(100, 1), (90, 1), (200, 3)], [(100, 60), (90, 1), (200, 150)]):
+        x = _setup(lens, 4, 2, 64, 16, dtype, seed=51)
+        for r in (1, 2):
+            x["table"][r][:4] = x["table"][0][:4]
+        x["table"][2][6] = x["table"][2][5]
+        _check(x, *_run(x))
+
+
 @pytest.mark.parametrize("dtype,Hq,Hkv,D,page", [(BF, 8, 2, 128, 16), (F32, 4, 4, 64, 32)])
 def test_serving_steps_match_whole_sequences(dtype, Hq, Hkv, D, page):
     """Three requests served in steps of chunks, drafts and single tokens (one joins late, one waits for pages once)
