@@ -12,6 +12,7 @@ constexpr int64_t kRowsW = kCUs * kRowsEU;
 template <int D>
 struct RowsLds {
   static constexpr int PER = kRowsNW;
+  static constexpr bool kOwnWords = true;
   float (*parts)[16 * D], (*stat)[16];
   __device__ __forceinline__ float* part(int w) const { return parts[w]; }
   __device__ __forceinline__ float* words(int w) const { return parts[w]; }

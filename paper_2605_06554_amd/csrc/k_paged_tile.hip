@@ -19,6 +19,7 @@
 // workgroup and two of them a CU (829 became 1150).
 #include <math.h>
 
+#include "lh_paged_lds.h"
 #include "lh_paged_rows.h"
 
 namespace lh {
@@ -32,15 +33,18 @@ struct TileCfg {
   static constexpr int RPB = 512 / D;                       // rows of one
 };
 
-// The ring as the memory of rows_tile: two parts of 16 rows in each of its arrays, four waves' words.
+// The ring as the memory of rows_tile.
 template <int D, int NW>
 struct TileLds {
-  static constexpr int PER = NW < 8 ? NW : 8;
-  float* ring[4];
+  using M = TileLdsMap<D, NW>;
+  static_assert(M::sound(), "a wave's words and another's part may be in use at the same time");
+  static constexpr int PER = M::PER;
+  static constexpr bool kOwnWords = M::kOwnWords;
+  float* ring[M::ARRAYS];
   float (*stat)[16];
   __device__ __forceinline__ float* at(int i, int off) const { return (i == 0 ? ring[0] : i == 1 ? ring[1] : i == 2 ? ring[2] : ring[3]) + off; }
-  __device__ __forceinline__ float* part(int w) const { return at(w & 3, (w >> 2) * 16 * D); }
-  __device__ __forceinline__ float* words(int w) const { return NW <= 4 ? at(w, 0) : at(w >> 2, (w & 3) * 8 * D); }
+  __device__ __forceinline__ float* part(int w) const { return at(M::part_array(w), M::part_off(w)); }
+  __device__ __forceinline__ float* words(int w) const { return at(M::words_array(w), M::words_off(w)); }
   __device__ __forceinline__ float* ms(int w) const { return stat[w]; }
   __device__ __forceinline__ float* ls(int w) const { return stat[NW + w]; }
 };

@@ -68,8 +68,9 @@ struct RowsItem {
   int64_t slot;  // else where the part's rows go
 };
 
-// The NW waves of a workgroup on it. Lds: part(w), 16 D floats of wave w (PER of them at a time); words(w), 4 KB of a
-// wave alone until a barrier (or part(w) itself, where PER = NW); ms(w), ls(w), 16 floats each. Rows of a
+// The NW waves of a workgroup on it. Lds: part(w), 16 D floats of wave w (PER of them at a time); words(w), 8 D floats of a
+// wave alone, inside part(w) where kOwnWords (a wave that is done writes its part while others use their words), else
+// anywhere, and a barrier stands before the first part; ms(w), ls(w), 16 floats each. Rows of a
 // part are swizzled (16-byte chunk c of row n at c ^ n). TM: rows that a part has room for in the workspace.
 template <typename T, int D, int RT, int NW, bool NT, int TM, typename Lds>
 __device__ __forceinline__ void rows_tile(const PagedArgs& a, const RowsItem& it, const Lds& lds) {
@@ -196,8 +197,8 @@ __device__ __forceinline__ void rows_tile(const PagedArgs& a, const RowsItem& it
   // words go through the wave's part of the LDS, and the columns are a loop that is not unrolled.
   auto odd_values = [&](int j0) __attribute__((always_inline)) {
     uint32_t* const mine = reinterpret_cast<uint32_t*>(lds.words(w)) + lane;
-    constexpr int HW = C::VW / 2;  // words of a key at a time: 4 KB a wave
-    static_assert(C::NV * HW * 64 * 4 <= 4096, "the words fit");
+    constexpr int HW = C::VW / 2;  // words of a key at a time: 32 D bytes a wave
+    static_assert(C::NV * HW * 64 * 4 <= 32 * D, "the words fit");
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
@@ -337,7 +338,8 @@ __device__ __forceinline__ void rows_tile(const PagedArgs& a, const RowsItem& it
 
   // ---- the waves joined, PER of them at a time
   constexpr int PER = Lds::PER;
-  if constexpr (PER < NW) __syncthreads();  // no wave needs its words any more
+  static_assert(Lds::kOwnWords ? PER == NW : true, "every wave has a part of its own");
+  if constexpr (!Lds::kOwnWords) __syncthreads();  // no wave needs its words any more
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float l = s.l[rt];

@@ -332,6 +332,43 @@ def test_infinite_values_that_rows_see(lens, dtype):
         assert bool(torch.isnan(o[:x["rows"], half:, 2:4]).all()) and bool((o[:x["rows"], half:, D - 1] == inf).all())
 
 
+def _waves(T, G, R):
+    """Waves of a workgroup of the tile kernel (bf16) for a step's rows a request."""
+    rows = T * G // R
+    assert rows > 32
+    wide = rows > 256 and -(-rows // 384) * 384 * 32 <= -(-rows // 256) * 256 * 33
+    return 4 if rows <= 112 else 12 if wide else 8
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("waves,chunk", [(4, 261), (8, 901), (12, 1349)])
+def test_odd_values_in_the_last_keys_of_small_tiles(waves, chunk, D, bad):
+    """A chunk whose last tile has 10 rows, beside requests of one to three tokens whose last block of 32 keys falls to
+    each wave in turn: a value of V among the last keys that is not finite reaches the rows that see its key, in
+    its column, and nothing else."""
+    print(f"[attend odd, small tiles] {waves} waves D={D} {bad}", flush=True)
+    for first in (0, 8):  # blocks before the last one
+        small = [(32 * (first + i) + (3, 29, 15, 20)[i % 4], 1 + i % 3) for i in range(8)]
+        lens = [(300, chunk)] + small
+        assert _waves(sum(n for _, n in lens), 2, len(lens)) == waves and chunk * 2 % (32 * waves) == 10
+        x = _setup(lens, 4, 2, D, 16, BF, seed=61 + first)
+        clean_o, clean_l = _run(x)
+        y, col = dict(x, vp=x["vp"].clone()), 5
+        sees = torch.zeros(x["T"], dtype=torch.bool, device=DEV)
+        for r, (old, n) in enumerate(lens):
+            p = old + n - 1 - (3 if r == 0 else 1 if n == 3 else 0)
+            y["vp"][x["table"][r][p // 16], 0, p % 16, col] = bad
+            sees[x["cu"][r] + p - old:x["cu"][r + 1]] = True
+        want = clean_o.clone()
+        want[sees, :2, col] = bad
+        for again in range(3):
+            o, lse = _run(y)
+            same = (o == want) | (torch.isnan(o) & torch.isnan(want))
+            assert bool(same.all()), f"{int((~same).sum())} elements, first {tuple(map(int, (~same).nonzero()[0]))}"
+            assert torch.equal(lse, clean_l)
+
+
 def test_large_logits():
     """Logits in the thousands, where a weight is 0 or 1, and runs of growing maxima."""
     print("[attend large logits]", flush=True)
