@@ -307,7 +307,7 @@ lh_status lh_attention_bwd_indexed(const lh_problem* pr, const void* q, const vo
    q, k and v may have a stride from token to token (slices of a fused projection), in elements, a
    multiple of 16 bytes and at least H * D. An output that overlaps another array of the call is refused (LH_E_PARAM):
    a loop that keeps kv_len as the next step's cached, or counts n_free down, copies between the calls. Bounds with
-   R * (T * Hq + 16 * Hkv) * (max_blocks * page + T + 1024) above 2^62 are refused. */
+   R * (T * Hq + 16 * Hkv) * (max_blocks * page + T * ceil(Hq / Hkv / 16) + 1024) above 2^62 are refused. */
 typedef struct {
   int32_t R;           /* requests of a step, 1 .. 4096                                            */
   int32_t max_blocks;  /* columns of the table, >= 1: a request holds max_blocks * page tokens      */

@@ -32,11 +32,14 @@ lh_status make_paged(const lh_paged* pc, LhPaged* s) {
   if (pc->max_blocks > k1G / pc->page)
     return lh_fail(LH_E_SHAPE, "a request could hold %d * %d > 2^30 tokens", pc->max_blocks, pc->page);
   if (pc->T > k1G / pc->Hq) return lh_fail(LH_E_SHAPE, "T * Hq = %lld * %d > 2^30", (long long)pc->T, pc->Hq);
-  // (units of the cut of an attention's work, whatever cu_q and kv_len hold: rows of 16 heads and up, keys in 16ths)
+  // The units of the cut of an attention's work (lh_paged_sdpa.h: Req) are counted in 64 bits, whatever cu_q and kv_len
+  // hold, each request clipped into [0, T) rows of its own: tiles of 16 rows and up, and a tile's keys, which for the
+  // G > 16 heads of a group grow by one a tile and not one a token.
+  const int64_t G = pc->Hq / pc->Hkv, grow = pc->T * ((G + 15) / 16);
   const unsigned __int128 units = (unsigned __int128)pc->R * (uint64_t)(pc->T * pc->Hq + 16 * (int64_t)pc->Hkv) *
-                                  (uint64_t)((int64_t)pc->max_blocks * pc->page + pc->T + 1024);
+                                  (uint64_t)((int64_t)pc->max_blocks * pc->page + grow + 1024);
   if (units > ((unsigned __int128)1 << 62))
-    return lh_fail(LH_E_SHAPE, "R * (T * Hq + 16 * Hkv) * (max_blocks * page + T + 1024) is above 2^62");
+    return lh_fail(LH_E_SHAPE, "R * (T * Hq + 16 * Hkv) * (max_blocks * page + T * ceil(Hq / Hkv / 16) + 1024) is above 2^62");
   memset(s, 0, sizeof(*s));
   s->T = pc->T, s->pages = pc->pages, s->R = pc->R, s->max_blocks = pc->max_blocks, s->page = pc->page;
   while ((1 << s->shift) < s->page) ++s->shift;

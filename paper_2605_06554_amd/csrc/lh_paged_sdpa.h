@@ -85,7 +85,8 @@ struct Req {
     const int32_t rest = rows - (tiles - 1) * TM;  // of the last tile
     lastw = NR > 0 && rest <= 16 ? NR : FW + ((16 - FW) * rest + TM - 1) / TM;
   }
-  // Units of tile t: the keys up to its last row (by whole tokens) and a constant, in 16ths.
+  // Units of tile t: the keys up to its last row (by whole tokens; where a token has several tiles, each counts as one:
+  // the host's bound on the sum allows for it) and a constant, in 16ths.
   __device__ __forceinline__ int64_t step(const PagedArgs& a) const { return a.G < TM ? TM / a.G : 1; }
   __device__ __forceinline__ int64_t past() const { return base > 0 ? base : 0; }
   __device__ __forceinline__ int64_t units(const PagedArgs& a, int64_t t) const {

@@ -1,5 +1,6 @@
 """The paged calls' refusals, on the host: nothing is launched by any of them."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -38,6 +39,45 @@ def test_check_codes(kw, code):
             lh.lh_paged_workspace_bytes(pc)
     else:
         assert lh.lh_paged_workspace_bytes(pc) >= 0
+
+
+def _units(pc, TM):
+    """The units of the cut (csrc/lh_paged_sdpa.h: Req) where every request's rows are clipped to all T and its keys to all
+    that its table row holds, in exact integers; lastw and the constant at their largest."""
+    G = pc.Hq // pc.Hkv
+    past, step, over = pc.max_blocks * pc.page, TM // G if G < TM else 1, 160
+    tiles = -(-pc.T * G // TM)
+    before = 16 * ((tiles - 1) * (past + over) + step * (tiles - 1) * tiles // 2)
+    return pc.R * pc.Hkv * (before + 16 * (past + tiles * step + over))
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(R=4096, T=2 ** 14, Hq=2 ** 16, Hkv=1, max_blocks=1, dtype=torch.float32), -2),  # 2^25 tiles a request: 2^65 units
+    (dict(R=4096, T=2 ** 14, Hq=2 ** 16, Hkv=1, max_blocks=1), -2),
+    (dict(R=4096, T=2 ** 20, Hq=2 ** 10, Hkv=2, max_blocks=1), -2),
+    (dict(R=1, T=2 ** 14, Hq=2 ** 16, Hkv=1, max_blocks=1, dtype=torch.float32), 0),
+    (dict(R=4096, T=4096, Hq=128, Hkv=1, max_blocks=2 ** 18), 0),
+    (dict(R=4096, T=2 ** 16, Hq=64, Hkv=1, max_blocks=2 ** 16), 0),
+])
+def test_units_of_the_cut_fit_64_bits(kw, code):
+    pc = _pc(**kw)
+    assert lh.lh_paged_check(pc) == code
+    if code == 0:
+        assert max(_units(pc, TM) for TM in (16, 32, 128, 256, 384)) < 2 ** 63
+
+
+def test_units_of_the_cut_fit_64_bits_wherever_the_check_passes():
+    rng = random.Random(9)
+    passed = near = 0
+    for _ in range(20000):
+        two = lambda hi: 2 ** rng.uniform(0, hi)  # noqa: E731
+        Hkv = int(two(8))
+        pc = _pc(R=int(two(12)), T=int(two(30)), Hkv=Hkv, Hq=Hkv * int(two(18)), max_blocks=int(two(26)))
+        if lh.lh_paged_check(pc) == 0:
+            most = max(_units(pc, TM) for TM in (16, 32, 128, 256, 384))
+            assert most < 2 ** 63, (pc, most)
+            passed, near = passed + 1, near + (most > 2 ** 58)
+    assert passed > 3000 and near > 20, (passed, near)
 
 
 def test_null_and_misaligned_pointers():
