@@ -322,7 +322,8 @@ typedef struct {
 
 /* Validates the bounds of a step (the rules above). Host only. */
 lh_status lh_paged_check(const lh_paged* pc);
-/* Bytes of device workspace that lh_sdpa_paged needs for steps of these bounds. Host only. */
+/* Bytes of device workspace that lh_sdpa_paged needs for steps of these bounds, and of every smaller R and T
+   beside the same heads, D and dtype: up to 103 MB. Host only. */
 lh_status lh_paged_workspace_bytes(const lh_paged* pc, size_t* bytes);
 
 /* Block tables, slot maps and lengths of a step. Request r has cached[r] tokens in the cache (the

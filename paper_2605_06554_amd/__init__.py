@@ -591,8 +591,8 @@ def _on(stream):
 
 
 def paged_workspace(pc, device="cuda"):
-    """A device byte buffer of lh_paged_workspace_bytes(pc) bytes. Calls that may run at the same time (two
-    streams, two captured graphs) need one each."""
+    """A device byte buffer of lh_paged_workspace_bytes(pc) bytes, enough for steps of fewer requests or rows too. Calls
+    that may run at the same time (two streams, two captured graphs) need one each."""
     return torch.empty(max(lh_paged_workspace_bytes(pc), 1), dtype=torch.uint8, device=device)
 
 

@@ -114,13 +114,13 @@ __global__ void __launch_bounds__(256) paged_join(const PagedArgs a, int TM) {
 // and 384: 16 rows 98 (16 a tile), 106, 119, 127; 48 128, 112, 119, 125; 96 291, 125, 126, 132; 128 201, 134, 130, 137;
 // 256 349, 194, 176, 182; 384 537, 329, 291, 233; 512 664, 346, 306, 348; 1024 1293, 628, 577, 628; one request of
 // 8192 rows 672, 358, 321, 318. Between 256 and 384 the rows that the last tile leaves idle decide.
-static PagedVariant variant_of(const LhPaged& s) {
-  const int64_t rows = s.T * s.G / s.R;
+static PagedVariant variant_of(const LhPaged& s, int64_t rows) {
   if (s.dtype != LH_BF16 || rows <= 32) return lh_paged_rows_variant(s, rows);
   if (rows <= 112) return lh_paged_tile_variant(s, 4);
   const int64_t in8 = (rows + 255) / 256 * 256, in12 = (rows + 383) / 384 * 384;
   return lh_paged_tile_variant(s, rows > 256 && in12 * 32 <= in8 * 33 ? 12 : 8);
 }
+static PagedVariant variant_of(const LhPaged& s) { return variant_of(s, s.T * s.G / s.R); }
 
 template <typename T, int D, bool SMALL>
 static void launch_join(const LhPaged& s, const PagedArgs& a, int TM, hipStream_t st) {
@@ -137,9 +137,17 @@ static void launch_join(const LhPaged& s, const PagedArgs& a, int TM, hipStream_
 
 using namespace lh;
 
+// The most that a step of up to R requests and T rows needs. (Steps of fewer requests or rows may take a variant of larger
+// parts, and one workspace serves them all.) The variants by the fewest rows a request that select them.
 size_t lh_sdpa_paged_ws_bytes(const LhPaged& s) {
-  const PagedVariant v = variant_of(s);
-  return paged_ws(v.W, v.TM, s.D).total;
+  size_t most = 0;
+  for (const int64_t rows : {1, 17, 33, 113, 257}) {
+    if (rows > 1 && rows > s.T * s.G) break;
+    const PagedVariant v = variant_of(s, rows);
+    const size_t bytes = paged_ws(v.W, v.TM, s.D).total;
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 
 hipError_t lh_launch_sdpa_paged(const LhPaged& s, const void* q, int64_t q_stride, const void* kpages,

@@ -80,6 +80,18 @@ def test_units_of_the_cut_fit_64_bits_wherever_the_check_passes():
     assert passed > 3000 and near > 20, (passed, near)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 8, 128), (8, 2, 64), (32, 8, 128), (64, 1, 128), (400, 1, 64)])
+def test_a_workspace_serves_smaller_steps(Hq, Hkv, D, dtype):
+    """One workspace for the largest R and T: no step of fewer requests or rows needs more."""
+    sizes = lambda: [1, 2, 3, 4, 7, 8, 9, 16, 32, 33, 64, 96, 97, 128, 256, 257, 384, 512, 1000, 4096]  # noqa: E731
+    need = {(R, T): lh.lh_paged_workspace_bytes(_pc(R=R, T=T, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype)) for R in sizes() for T in sizes()}
+    for a, b in zip(sizes(), sizes()[1:]):
+        for x in sizes():
+            assert need[a, x] <= need[b, x] and need[x, a] <= need[x, b], (a, b, x)
+    assert max(need.values()) <= 103 << 20
+
+
 def test_null_and_misaligned_pointers():
     lib, pc = lh._load(), _pc()
     ok = [0x10000 * (i + 1) for i in range(12)]
