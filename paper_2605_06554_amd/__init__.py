@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 
 import torch
@@ -430,6 +431,22 @@ def _need_on(fn, t, name, dt, n, dev):
     raise LighthouseError(f"{fn}: {name} has {t.numel()} elements, {n} needed")
 
 
+def _need_laid(fn, t, name, dt, full, dev):
+    """_need_on, of a tensor laid out as `full` (or with more of the first, or as many elements in one run): the elements
+    in rows of another length, or in another order, would be read as other pages and tokens."""
+    try:
+        if t.shape == full and t.dtype is dt and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        if t is None or isinstance(t, int):
+            return t
+        raise
+    at = _need_on(fn, t, name, dt, math.prod(full), dev)
+    if len(t.shape) == len(full) and t.shape[1:] != full[1:]:
+        raise LighthouseError(f"{fn}: {name} has shape {tuple(t.shape)}, rows of {full[1:]} needed")
+    return at
+
+
 def _need_rows(fn, t, name, dt, T, H, D, dev):
     """[T, H, D] (or more rows) whose rows of H * D elements are dense: its address and the stride between them, in
     elements."""
@@ -458,7 +475,7 @@ def lh_page_plan(pc, cached, fresh, free_pages, n_free, table, cu_q, kv_len, slo
     R, T = pc.R, pc.T
     _call(fn, ctypes.byref(pc), need(fn, cached, "cached", i32, R, dev), need(fn, fresh, "fresh", i32, R, dev),
           need(fn, free_pages, "free_pages", i32, pc.pages, dev), need(fn, n_free, "n_free", i32, 1, dev),
-          need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
+          _need_laid(fn, table, "table", i32, (R, pc.max_blocks), dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
           need(fn, kv_len, "kv_len", i32, R, dev), need(fn, slots, "slots", i32, T, dev), need(fn, pos, "pos", i32, T, dev),
           need(fn, balance, "balance", i32, 1, dev), need(fn, n_taken, "n_taken", i32, 1, dev), _stream(stream, dev))
 
@@ -467,21 +484,23 @@ def lh_page_write(pc, k, v, slots, kpages, vpages, stream=None):
     """The strides of the C entry point are k's and v's own."""
     fn, dt, dev, need = "lh_page_write", _xdt(pc), _device(), _need_on
     T, H, D = pc.T, pc.Hkv, pc.D
-    n = pc.pages * H * pc.page * D
+    pool = (pc.pages, H, pc.page, D)
     kp, ks = _need_rows(fn, k, "k", dt, T, H, D, dev)
     vp, vs = _need_rows(fn, v, "v", dt, T, H, D, dev)
     _call(fn, ctypes.byref(pc), kp, ks, vp, vs, need(fn, slots, "slots", torch.int32, T, dev),
-          need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev), _stream(stream, dev))
+          _need_laid(fn, kpages, "kpages", dt, pool, dev), _need_laid(fn, vpages, "vpages", dt, pool, dev),
+          _stream(stream, dev))
 
 
 def lh_sdpa_paged(pc, q, kpages, vpages, table, cu_q, kv_len, o, lse, ws, ws_bytes=None, stream=None):
     """The stride of the C entry point is q's own; lse may be None."""
     fn, dt, i32, dev, need = "lh_sdpa_paged", _xdt(pc), torch.int32, _device(), _need_on
     R, T, H, D = pc.R, pc.T, pc.Hq, pc.D
-    n = pc.pages * pc.Hkv * pc.page * D
+    pool = (pc.pages, pc.Hkv, pc.page, D)
     qp, qs = _need_rows(fn, q, "q", dt, T, H, D, dev)
-    _call(fn, ctypes.byref(pc), qp, qs, need(fn, kpages, "kpages", dt, n, dev), need(fn, vpages, "vpages", dt, n, dev),
-          need(fn, table, "table", i32, R * pc.max_blocks, dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
+    _call(fn, ctypes.byref(pc), qp, qs, _need_laid(fn, kpages, "kpages", dt, pool, dev),
+          _need_laid(fn, vpages, "vpages", dt, pool, dev),
+          _need_laid(fn, table, "table", i32, (R, pc.max_blocks), dev), need(fn, cu_q, "cu_q", i32, R + 1, dev),
           need(fn, kv_len, "kv_len", i32, R, dev), need(fn, o, "o", dt, T * H * D, dev),
           need(fn, lse, "lse", torch.float32, T * H, dev), need(fn, ws, "ws", torch.uint8, ws_bytes or 0, dev),
           _nbytes(ws) if ws_bytes is None else ws_bytes, _stream(stream, dev))

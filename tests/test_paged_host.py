@@ -228,6 +228,24 @@ def test_binding_refuses_bad_tensors():
         _refused(lh.lh_sdpa_paged, attend, i, bad, msg)
 
 
+def test_binding_refuses_other_layouts():
+    """As many elements in table rows of another width, or in pages laid out otherwise."""
+    pc, i32, bf = _pc(), torch.int32, torch.bfloat16
+    plan = [pc, _Fake([4], i32), _Fake([4], i32), _Fake([64], i32), _Fake([1], i32), _Fake([4, 8], i32), _Fake([5], i32),
+            _Fake([4], i32), _Fake([100], i32), _Fake([100], i32), _Fake([1], i32)]
+    pool = _Fake([64, 2, 16, 64], bf)
+    write = [pc, _Fake([100, 2, 64], bf), _Fake([100, 2, 64], bf), _Fake([100], i32), pool, pool]
+    attend = [pc, _Fake([100, 8, 64], bf), pool, pool, _Fake([4, 8], i32), _Fake([5], i32), _Fake([4], i32),
+              _Fake([100, 8, 64], bf), _Fake([100, 8], torch.float32), _Fake([1 << 30], torch.uint8)]
+    for call, args, at in ((lh.lh_page_plan, plan, 5), (lh.lh_sdpa_paged, attend, 4)):
+        for shape in ([4, 9], [4, 16], [8, 4]):
+            _refused(call, args, at, _Fake(shape, i32), "table has shape .* rows of")
+    for call, args, ats in ((lh.lh_page_write, write, (4, 5)), (lh.lh_sdpa_paged, attend, (2, 3))):
+        for at in ats:
+            for shape in ([64, 16, 2, 64], [32, 2, 32, 64], [64, 4, 16, 64]):
+                _refused(call, args, at, _Fake(shape, bf), "pages has shape .* rows of")
+
+
 def test_reference_plan_hands_out_pages_in_order():
     """The oracle of the plan itself, on a case worked by hand: pages of 16; request 0 fills its page and takes one;
     request 1 brings nothing; request 2 lacks pages and waits; request 3 needs none and goes on; request 4 waits."""
