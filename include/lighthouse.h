@@ -337,10 +337,12 @@ lh_status lh_paged_workspace_bytes(const lh_paged* pc, size_t* bytes);
      - cu_q[r], the sum of the fresh counts before r (clipped at T), r = 0 .. R;
      - kv_len[r] = cached[r] + fresh[r], or 0 for a request that waits;
      - slots[t] and pos[t] of the tokens, -1 where the request waits and behind the last request;
-     - n_taken[0] (may be NULL), the pages taken: free_pages[0 .. n_free[0] - n_taken[0]) are still free;
+     - n_taken[0], the pages taken: free_pages[0 .. n_free[0] - n_taken[0]) are still free, and that difference
+       is the next step's n_free (NULL only for a caller that does not go on with this stack);
      - balance[0] = n_free[0] less the pages that the requests up to the last admitted one ask for, those that
-       wait for pages among them: what is left, n_free[0] - n_taken[0], unless a request was admitted behind
-       one that waits for pages; then less, and below 0 by the pages that the waiting ones lack.
+       wait for pages among them: n_free[0] - n_taken[0], unless a request was admitted behind one that
+       waits for pages; then less, and below 0 by the pages that the waiting ones lack. A measure of how short the pool
+       is, not a count of free pages: kept as the next n_free it leaves pages unused.
    free_pages holds `pages` entries; n_free[0] outside [0, pages] counts as the nearest end. A page
    id of free_pages or table outside [0, pages) gives the slot -1. */
 lh_status lh_page_plan(const lh_paged* pc, const int32_t* cached, const int32_t* fresh,

@@ -622,7 +622,8 @@ def paged_cache(pages, page, Hkv, D, dtype=torch.bfloat16, device="cuda"):
 
 def page_plan(pc, cached, fresh, free_pages, n_free, table, stream=None):
     """Allocates the outputs and runs lh_page_plan. Returns a dict of cu_q, kv_len, slots, pos, balance and n_taken;
-    the new entries of table are written in place. The next step's n_free is this one's less n_taken."""
+    the new entries of table are written in place. The next step's n_free is this one's less n_taken (not balance, which
+    counts the pages of waiting requests too)."""
     e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)  # noqa: E731
     with _on(stream):
         out = dict(cu_q=e(pc.R + 1), kv_len=e(pc.R), slots=e(pc.T), pos=e(pc.T), balance=e(1), n_taken=e(1))

@@ -1,5 +1,7 @@
 """The paged calls on the GPU against their definitions (paged_ref.py): the plan and the write exactly, the attention
 within the bound that its arithmetic allows."""
+import importlib.util
+import os
 import random
 
 import pytest
@@ -83,6 +85,54 @@ def test_plan_of_large_lengths():
     ref = paged_ref.plan(cached, fresh, list(range(64)), 64, [[9, -1, -1, -1]] * R, 16, 64, 40)
     for got, want in zip((tab, out["cu_q"], out["kv_len"], out["slots"], out["pos"]), ref):
         assert torch.equal(got.cpu(), torch.tensor(want, dtype=I32))
+
+
+def _timed_cases():
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "perf", "operators.py")
+    spec = importlib.util.spec_from_file_location("timed_operators", at)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    return mod
+
+
+@pytest.mark.parametrize("spare", [1.3, 1.0, 0.9, 0.6, 0.2])
+def test_plan_of_the_timed_ranges(spare):
+    """The timed plans, and such with a pool that runs short, against their definition there; the pages left are
+    n_free - n_taken (requests that need no page are admitted behind those that wait for some)."""
+    m = _timed_cases()
+    cases = [c for c in m.listed() if c["kind"] == "plan"]
+    cases += [m._case("plan", R, (1, 300), (0, 5000), page=page, ones=0.5) for R, page in ((7, 16), (33, 64), (200, 256))]
+    for c in cases:
+        c = dict(c, spare=spare)
+        print(f"[plan timed] R={c['R']} page={c['page']} spare={spare}", flush=True)
+        s, want = m.prepare(c, 5), m.exact(c, 5)
+        pc = lh.paged(c["R"], s["width"], s["T"], s["pages"], c["page"], c["Hq"], c["Hkv"], c["D"])
+        out = lh.page_plan(pc, s["old"], s["new"], s["free"], s["n_free"], s["table"])
+        got = dict(table=s["table"], n_left=s["n_free"] - out["n_taken"], **{n: out[n] for n in ("cu_q", "kv_len", "slots", "pos")})
+        for name in want:
+            assert torch.equal(got[name], want[name]), name
+
+
+def test_every_free_page_is_handed_out():
+    """A pool that runs short, over steps that go on with n_free - n_taken: a long request waits while others go on, and
+    in the end no page is left."""
+    print("[plan] every page", flush=True)
+    page, pages, width, T = 16, 30, 40, 512
+    pc = lh.paged(3, width, T, pages, page, 2, 2, 64)
+    free, table = list(range(pages)), [[-1] * width for _ in range(3)]
+    tab, n_free, cached = _i(table), pages, [0, 0, 0]
+    ids, n_free_t = _i(free), _i([pages])
+    for step in range(40):
+        fresh = [15, 470 if step else 1, 1 if step < 16 else 0]
+        out = lh.page_plan(pc, _i(cached), _i(fresh), ids, n_free_t, tab)
+        table, _, kv, _, _, left, balance = paged_ref.plan(cached, fresh, free, n_free, table, page, pages, T)
+        assert torch.equal(tab.cpu(), torch.tensor(table, dtype=I32)) and out["kv_len"].tolist() == kv
+        n_free_t = n_free_t - out["n_taken"]
+        n_free = left
+        assert int(n_free_t) == left and (balance < left) == (step > 0)
+        cached = [k or c for k, c in zip(kv, cached)]
+    held = [i for r in range(3) for i in table[r][:paged_ref.blocks(cached[r], page)]]
+    assert n_free == 0 and sorted(held) == free
 
 
 # ------------------------------------------------------------------ write
