@@ -360,7 +360,9 @@ lh_status lh_page_write(const lh_paged* pc, const void* k, int64_t k_stride, con
 /* Attention of the step's rows over the cache: row cu_q[r] + i of request r, whose position is
    kv_len[r] - (cu_q[r+1] - cu_q[r]) + i, attends to the request's tokens up to that position:
    o = softmax(scale q K^T) V and lse, the natural-log log-sum-exp of its scaled logits
-   (may be NULL). Logits, statistics and sums in fp32. A row without a token (a request that waits) gets o = 0
+   (may be NULL). Logits, statistics and sums in fp32. In bf16, where a step has more than 32 rows a request
+   (T * Hq / Hkv / R), the weights of tiles of more than 16 rows are rounded to bf16 (by up to 2^-8 of themselves) for their
+   product with V; elsewhere o is off by little more than its own rounding. A row without a token (a request that waits) gets o = 0
    and lse = -inf. Cached rows that no query row may see (behind kv_len, of other requests, after
    the row itself) have no effect on it, whatever they hold. Entries of table outside
    [0, pages) and lengths beyond the table are clamped (no out-of-range read; what such a

@@ -55,6 +55,9 @@ static PagedVariant variant() {
 }
 // A request of one tile reads its keys once, and the non-temporal hint is worth 8% of the time (6.1 against 5.6
 // TB/s, 64 requests of 482,000 keys); one of several finds them in the caches (four tiles, fp32: 60 us, 67 with the hint).
+// fp32 takes 32 rows a tile above 16 whatever the number of tiles: 39 us where 16 rows take 42 (8 requests of 16 tokens at 4000,
+// 8 heads on 2), 69 and 70 (16 of 40 at 1000, 8 on 8); few and short ones lose by it, 30 and 20 (3 of 12 at 2200, 8 on 2).
+// At D = 128 it spills 16 registers, outside the loop over the keys.
 template <typename T, int D>
 static PagedVariant variant(int64_t rows) {
   return rows > 32 ? variant<T, D, 2, false>() : rows > 16 ? variant<T, D, 2, true>() : variant<T, D, 1, true>();

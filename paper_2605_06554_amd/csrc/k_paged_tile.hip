@@ -3,13 +3,19 @@
 //
 // The arithmetic and the LDS tiles are those of the layer's forward kernel (k_sdpa_mfma.hip: layouts,
 // swizzle, two-slot ring filled by global_load_lds): S^T = K Q^T, a lane owning one row, 64 keys a tile; P is
-// rounded to bf16 for its product, everything else of the softmax is fp32. What differs:
+// rounded to bf16 for its product, everything else of the softmax is fp32. (The roundings are independent and no larger than
+// that of o itself, so the 2-norm error is at most sqrt(2) of the output's where V has no common sign: 2.0e-3 to 2.4e-3, and
+// 1.7e-3 with P as two bf16 values, as in lh_paged_rows.h. Here the matrix unit has no time to spare for the second
+// product: the chunk below takes 1150 us with it and 858 without, two prompts of 7000 to 8192 tokens 645 and 500.)
+// What differs:
 //   - A tile of 64 keys is filled page by page: the 4 or 8 rows that one load instruction copies lie in one
 //     page (pages hold 16 tokens or more), so their address is one scalar base, read from the table a tile
 //     ahead, and a fixed offset a lane. The tile with the request's last key reads that key again for the
 //     rows behind it, which hold anything.
 //   - The keys of a tile are a part's share of them, and the rows of a part of a tile go to the workspace.
 //   - Rows whose mask leaves nothing, and values of V that are not finite: what is masked does not reach a row.
+// 12 waves have 168 registers each: at D = 128 they spill 5, two of which are read again in every masked tile (1 without MIX, read
+// once); the others spill none.
 //
 // Bound by the matrix and vector units side by side, at a clock that their power sets (1.7 to 2.0 GHz): a chunk of 2048
 // tokens at 96,000 cached, 8 heads of 128, 256 rows a tile: 835 to 870 us, 940 to 980 TFLOP/s (a large library product
