@@ -442,7 +442,8 @@ def _need_laid(fn, t, name, dt, full, dev):
             return t
         raise
     at = _need_on(fn, t, name, dt, math.prod(full), dev)
-    if len(t.shape) == len(full) and t.shape[1:] != full[1:]:
+    several = full[0] if len(full) == 2 else full[1]  # (one request's row of the table, or one head's tokens, lie as they do)
+    if several > 1 and len(t.shape) == len(full) and t.shape[1:] != full[1:]:
         raise LighthouseError(f"{fn}: {name} has shape {tuple(t.shape)}, rows of {full[1:]} needed")
     return at
 

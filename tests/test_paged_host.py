@@ -246,6 +246,16 @@ def test_binding_refuses_other_layouts():
                 _refused(call, args, at, _Fake(shape, bf), "pages has shape .* rows of")
 
 
+def test_binding_takes_layouts_that_are_the_same_memory():
+    """A wider table of one request, pages of one head in another order, and one run of elements, are read as before."""
+    i32, bf, need = torch.int32, torch.bfloat16, lh._need_laid
+    for shape, dt, full in (([1, 9], i32, (1, 8)), ([4, 9], i32, (1, 8)), ([32], i32, (4, 8)), ([5, 8], i32, (4, 8)),
+                            ([64, 16, 1, 64], bf, (64, 1, 16, 64)), ([32, 1, 32, 64], bf, (64, 1, 16, 64)),
+                            ([65, 2, 16, 64], bf, (64, 2, 16, 64)), ([64 * 2 * 16 * 64], bf, (64, 2, 16, 64))):
+        assert need("f", _Fake(shape, dt), "x", dt, full, 0) == 0x1000
+    assert need("f", None, "x", i32, (1, 8), 0) is None and need("f", 4096, "x", i32, (1, 8), 0) == 4096
+
+
 def test_reference_plan_hands_out_pages_in_order():
     """The oracle of the plan itself, on a case worked by hand: pages of 16; request 0 fills its page and takes one;
     request 1 brings nothing; request 2 lacks pages and waits; request 3 needs none and goes on; request 4 waits."""
